@@ -290,8 +290,7 @@ def _call(s):
     if kind == "clip":
         vb.clip_gradients(grads, c["limit"], s["norm"], into=others, workspace=s["workspace"])
         return dict(norm=s["norm"], grads=_joined(s["others"]))
-    vb.gradient_norm(grads, c["limit"], s["norm"], workspace=s["workspace"])
-    vb.sgd_step_scaled(others, grads, 1e-3, s["norm"])
+    vb.sgd_step_clipped(others, grads, 1e-3, c["limit"], s["norm"], workspace=s["workspace"])
     return dict(norm=s["norm"], weights=_joined(s["others"]))
 
 
