@@ -470,6 +470,87 @@ int32_t varco_softmax_xent(varco_ctx* ctx, const void* logits, int64_t ld, const
  * averaging of the workers' parameters amounts to. */
 int32_t varco_sgd_step(void* w, const void* dw, int64_t n, float lr, varco_stream stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Normalised rows, 8-bit codes, products of codes, limited gradient steps: what deep or narrow-precision variants of the layers
+ * above add around their dense transforms. These calls belong to no context: sizes, types (VARCO_F32 or VARCO_BF16) and
+ * leading dimensions are arguments, failures are reported through varco_last_error(NULL). They allocate nothing, keep
+ * nothing from one call for the next, never synchronise and may be captured. Float matrices may start at any address of
+ * an element and have any leading dimension >= width. Where a call needs scratch memory the caller
+ * passes it: `workspace`, 256-byte aligned, of at least the bytes that the matching *_workspace call names for the same sizes;
+ * its contents matter neither before nor after, and it must not be shared by calls (or graphs) that may overlap. 0 bytes: NULL
+ * will do. Counts of rows are below 2^31, widths 1 .. VARCO_MAX_CODE_WIDTH.
+ *
+ * Codes. A row of `width` numbers is stored as `width` bytes of 4 exponent and 3 fraction bits (e4m3: largest 448, no infinity) and a
+ * scale 2^e for each 128 columns, a byte e + 127 (e8m0). a = the largest finite |v| of the block; e is the smallest integer with
+ * a 2^-e <= 448, but at least -127 (and 0 where a = 0); the code is v 2^-e rounded to the nearest code, ties to even; an infinity or
+ * NaN becomes a NaN code and does not take part in a. A power of two as scale moves no number inside the codes' range to
+ * another rounding than a scale 448 / a would, loses at most one of the 18 binades at its end, and is applied by the matrix units.
+ * Rows lie one after the other, VARCO_CODE_LD(width) code bytes and VARCO_SCALE_LD(width) scale bytes each; bytes behind the
+ * last column are 0 and 127 (written so by the calls that make codes, and expected so by those that take them). Codes
+ * start at a multiple of 16 bytes, scales at one of 4.
+ * A weight matrix has one scale for 128 x 128 elements: scale rows of its 128-row blocks. */
+#define VARCO_MAX_CODE_WIDTH 16384
+#define VARCO_CODE_LD(width) (((width) + 15) / 16 * 16)
+#define VARCO_SCALE_LD(width) (((width) + 511) / 512 * 4)
+
+/* Codes of n_rows rows of x. gate != NULL: of x where gate > 0 and 0 elsewhere (the errors behind a ReLU whose output is gate). */
+int32_t varco_quantize_rows(int32_t dtype, int64_t n_rows, int32_t width, const void* x, int64_t ldx, const void* gate, int64_t ldg,
+                            void* codes, void* scales, varco_stream stream);
+/* Codes of the fp32 weights h (n_in x n_out, leading dimension ldh), in either or both orientations, the same numbers:
+ *   turned  n_out rows of VARCO_CODE_LD(n_in), scales (blocks of n_out) x VARCO_SCALE_LD(n_in): what the forward product takes
+ *   codes   n_in rows of VARCO_CODE_LD(n_out), scales (blocks of n_in) x VARCO_SCALE_LD(n_out): what the input gradient takes
+ * A pair that is not wanted is NULL. */
+int32_t varco_quantize_weights(int32_t n_in, int32_t n_out, const void* h, int64_t ldh, void* turned, void* turned_scales, void* codes,
+                               void* scales, varco_stream stream);
+/* c = act((c +) X W), n_rows x n_out of type dtype, X of n_rows x n_in codes, W the n_in x n_out weights given as `turned` above
+ * (input gradients: X the codes of the errors, n_in the layer's outputs, W its `codes`). The products of the codes' values are exact. dtype VARCO_F32: sums
+ * as accurate as fp32 additions. VARCO_BF16: sums in fp32 of the 8-bit matrix units, which drop of each product what lies 2^-13 below the
+ * largest of the eight consecutive ones it is added with (an error below 2^-10 of the sum of the products' sizes, typically a tenth of the rounding
+ * of c), at twice the rate. One rounding to c. act: VARCO_ACT_*. accumulate != 0 adds to what c holds. c must not overlap an operand. */
+int32_t varco_scaled_transform(int32_t dtype, int64_t n_rows, int32_t n_in, int32_t n_out, const void* codes, const void* scales,
+                               const void* w_codes, const void* w_scales, void* c, int64_t ldc, int32_t accumulate, int32_t act,
+                               varco_stream stream);
+/* Weight gradient dh = Y^T D (accumulate != 0: added to what dh holds), fp32 n_in x n_out, from rows of codes of the inputs Y (width
+ * n_in) and of the errors D (width n_out), summed in fp32 in one order. n_rows = 0 gives 0. */
+int32_t varco_scaled_weight_workspace(int64_t n_rows, int32_t n_in, int32_t n_out, int64_t* bytes);
+int32_t varco_scaled_bwd_weight(int64_t n_rows, int32_t n_in, int32_t n_out, const void* y_codes, const void* y_scales, const void* d_codes,
+                                const void* d_scales, void* dh, int64_t ldh, int32_t accumulate, void* workspace, int64_t workspace_bytes,
+                                varco_stream stream);
+
+/* Root-mean-square norm, with the residual's addition:
+ *   u = x + residual, rounded to the storage type (u = x without one)     s = 1 / sqrt(mean of u^2 over the row + eps)
+ *   y[j] = u[j] s gain[j]
+ * residual, gain (fp32, NULL = 1), total, y, codes (with scales), inv_rms may be NULL; what is given is written: total = u, which
+ * the backward call reads, y in the storage type, the codes of y (from its fp32 values), inv_rms[row] = s (fp32). total and y may be
+ * x or the residual themselves (same leading dimension), not each other. */
+int32_t varco_rms_norm_fwd(int32_t dtype, int64_t n_rows, int32_t width, const void* x, int64_t ldx, const void* residual, int64_t ldr,
+                           const void* gain, float eps, void* total, int64_t ldt, void* y, int64_t ldy, void* codes, void* scales,
+                           void* inv_rms, varco_stream stream);
+/* Its backward pass, h = dy gain, v = u inv_rms:
+ *   dx = inv_rms (h - v mean(h v)) (+ dtotal)      dgain = sum over rows of dy v (accumulate != 0: added to what dgain holds)
+ * u, inv_rms as the forward call gave them. dx is the gradient of x and of the residual; dtotal (NULL: none) is what reaches u
+ * on other paths. dx or dgain may be NULL; dx may be dy, u or dtotal (same leading dimension). The rows' sums are added in one order. */
+int32_t varco_rms_norm_workspace(int32_t dtype, int64_t n_rows, int32_t width, int64_t* bytes);
+int32_t varco_rms_norm_bwd(int32_t dtype, int64_t n_rows, int32_t width, const void* dy, int64_t lddy, const void* u, int64_t ldu, const void* gain,
+                           const void* inv_rms, const void* dtotal, int64_t lddt, void* dx, int64_t lddx, void* dgain, int32_t accumulate,
+                           void* workspace, int64_t workspace_bytes, varco_stream stream);
+
+/* The norm of all gradients together, norm = sqrt(sum of g^2 over all elements of all tensors), summed in fp64 in one order, and the
+ * factor that limits it, f = min(1, max_norm / norm) (1 for norm = 0): out[0] = norm, out[1] = f (fp32, device).
+ * A NaN among the gradients makes both NaN, an infinity makes the norm infinite and f = 0.
+ *   varco_gradient_norm     norm and factor
+ *   varco_clip_gradients    into[t] = f grads[t]; into[t] may be grads[t]
+ *   varco_sgd_step_clipped  w[t] -= lr f dw[t], fp32
+ * grads, into, w, dw: host arrays of n_tensors device pointers; sizes: host array of element counts (0 is allowed). Tensors
+ * that are written must not overlap others. The arrays are read before the call returns. max_norm >= 0, infinity included. */
+int32_t varco_gradient_norm_workspace(int32_t n_tensors, const int64_t* sizes, int64_t* bytes);
+int32_t varco_gradient_norm(int32_t dtype, int32_t n_tensors, const void* const* grads, const int64_t* sizes, float max_norm, void* out,
+                            void* workspace, int64_t workspace_bytes, varco_stream stream);
+int32_t varco_clip_gradients(int32_t dtype, int32_t n_tensors, const void* const* grads, void* const* into, const int64_t* sizes, float max_norm,
+                             void* out, void* workspace, int64_t workspace_bytes, varco_stream stream);
+int32_t varco_sgd_step_clipped(int32_t n_tensors, void* const* w, const void* const* dw, const int64_t* sizes, float lr, float max_norm, void* out,
+                               void* workspace, int64_t workspace_bytes, varco_stream stream);
+
 /* Section IV / Appendix "Scheduler": the compression ratio of iteration `step` of `n_steps`, as an exact
  * rational num/den >= 1 for varco_set_ratio (host only, no device work). The ratio starts at c_max and never
  * increases; it is clamped at c_min >= 1.

@@ -21,6 +21,8 @@ ORDER_AGGREGATE_FIRST, ORDER_TRANSFORM_FIRST = 0, 1
 F32 = 0
 BF16 = 1
 MAX_LAYERS = 16
+MAX_CODE_WIDTH = 16384
+CODE_BLOCK = 128          # columns of a row of codes that share a scale
 
 EXPORTS = [
     "varco_partition_build", "varco_partition_view", "varco_partition_free",
@@ -36,6 +38,9 @@ EXPORTS = [
     "varco_network_aggregate_fwd", "varco_network_aggregate_bwd",
     "varco_network_taps_fwd", "varco_network_taps_bwd_weight", "varco_network_taps_bwd_input",
     "varco_network_taps_bwd_last_hop",
+    "varco_quantize_rows", "varco_quantize_weights", "varco_scaled_transform", "varco_scaled_weight_workspace",
+    "varco_scaled_bwd_weight", "varco_rms_norm_fwd", "varco_rms_norm_workspace", "varco_rms_norm_bwd",
+    "varco_gradient_norm_workspace", "varco_gradient_norm", "varco_clip_gradients", "varco_sgd_step_clipped",
 ]
 KERNEL_CLASSES = ["compress", "decompress", "agg_fwd", "gemm_fwd", "gemm_wgrad", "gemm_dgrad", "agg_bwd_local",
                   "agg_bwd_halo", "reduce", "agg_bwd_halo_sum"]
@@ -139,6 +144,19 @@ def lib() -> C.CDLL:
         L.varco_network_taps_bwd_weight.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp]
         L.varco_network_taps_bwd_input.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp]
         L.varco_network_taps_bwd_last_hop.argtypes = [vp, i32, vp, vp, vp, vp, C.POINTER(i32), vp]
+        f32 = C.c_float
+        L.varco_quantize_rows.argtypes = [i32, i64, i32, vp, i64, vp, i64, vp, vp, vp]
+        L.varco_quantize_weights.argtypes = [i32, i32, vp, i64, vp, vp, vp, vp, vp]
+        L.varco_scaled_transform.argtypes = [i32, i64, i32, i32, vp, vp, vp, vp, vp, i64, i32, i32, vp]
+        L.varco_scaled_weight_workspace.argtypes = [i64, i32, i32, C.POINTER(i64)]
+        L.varco_scaled_bwd_weight.argtypes = [i64, i32, i32, vp, vp, vp, vp, vp, i64, i32, vp, i64, vp]
+        L.varco_rms_norm_fwd.argtypes = [i32, i64, i32, vp, i64, vp, i64, vp, f32, vp, i64, vp, i64, vp, vp, vp, vp]
+        L.varco_rms_norm_workspace.argtypes = [i32, i64, i32, C.POINTER(i64)]
+        L.varco_rms_norm_bwd.argtypes = [i32, i64, i32, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp, i32, vp, i64, vp]
+        L.varco_gradient_norm_workspace.argtypes = [i32, vp, C.POINTER(i64)]
+        L.varco_gradient_norm.argtypes = [i32, i32, vp, vp, f32, vp, vp, i64, vp]
+        L.varco_clip_gradients.argtypes = [i32, i32, vp, vp, vp, f32, vp, vp, i64, vp]
+        L.varco_sgd_step_clipped.argtypes = [i32, vp, vp, vp, f32, f32, vp, vp, i64, vp]
         L.varco_profile_enable.argtypes = [vp, i32]
         L.varco_profile_read.argtypes = [vp, C.POINTER(Profile), i32]
         for name in EXPORTS:
@@ -203,6 +221,250 @@ def sum_gradients(dst, src, stream=None):
     """dst += src (fp32 device tensors of equal size)."""
     assert dst.numel() == src.numel() and dst.dtype == src.dtype
     _check(lib().varco_sum_gradients(_ptr(dst), _ptr(src), dst.numel(), _stream(stream)))
+
+
+# ---------------------------------------------------------------------------------------------------------
+# normalised rows, 8-bit codes and their products, limited gradient steps
+# ---------------------------------------------------------------------------------------------------------
+
+def code_ld(width: int) -> int:
+    """Bytes of a row of `width` codes (VARCO_CODE_LD of the header)."""
+    return (width + 15) // 16 * 16
+
+
+def scale_ld(width: int) -> int:
+    """Bytes of the scales of a row of `width` codes (VARCO_SCALE_LD of the header)."""
+    return (width + 511) // 512 * 4
+
+
+def _refuse(code, text):
+    raise VarcoError(code, text)
+
+
+def _dtype(t):
+    name = str(t.dtype)
+    if name == "torch.float32":
+        return F32
+    if name == "torch.bfloat16":
+        return BF16
+    _refuse(ERR_UNSUPPORTED, f"{name}: neither float32 nor bfloat16")
+
+
+def _on_device(*tensors):
+    """Tensors of a call are on the device that is current (a launch goes there, whatever device the memory is on)."""
+    import torch
+    current = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != current):
+            _refuse(ERR_INVALID_ARG, f"a tensor on {t.device}, the current device is cuda:{current}")
+
+
+def _matrix(t, shape, like, what):
+    """(address, leading dimension) of a matrix whose rows' elements are consecutive; None -> NULL."""
+    if t is None:
+        return None, 0
+    if t.dim() != 2 or tuple(t.shape) != shape:
+        _refuse(ERR_SHAPE, f"{what}: {tuple(t.shape)} where {shape} is needed")
+    if t.dtype != like:
+        _refuse(ERR_UNSUPPORTED, f"{what}: {t.dtype} where {like} is needed")
+    if shape[1] > 1 and t.stride(1) != 1:
+        _refuse(ERR_SHAPE, f"{what}: the elements of a row are not consecutive")
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else max(shape[1], 1)
+
+
+def _vector(t, n, what):
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous():
+        _refuse(ERR_SHAPE, f"{what}: {n} consecutive float32 values are needed")
+    return t.data_ptr()
+
+
+def _code_rows(codes, scales, rows, width, scale_rows, what):
+    """Addresses of rows of codes and of their scales: whole buffers of bytes (uint8, or the 8-bit float types)."""
+    if codes is None and scales is None:
+        return None, None
+    if codes is None or scales is None:
+        _refuse(ERR_INVALID_ARG, f"{what}: codes without scales")
+    for t, n, ld in ((codes, rows, code_ld(width)), (scales, scale_rows, scale_ld(width))):
+        if t.element_size() != 1 or tuple(t.shape) != (n, ld) or not t.is_contiguous():
+            _refuse(ERR_SHAPE, f"{what}: {tuple(t.shape)} where {n} whole rows of {ld} bytes are needed")
+    return codes.data_ptr(), scales.data_ptr()
+
+
+def _scratch(need, workspace, device, stream):
+    """(address, bytes, tensor to hold) of a call's scratch memory: the caller's, or a new one that torch's allocator keeps for work of
+    the call's stream."""
+    if workspace is None:
+        if need == 0:
+            return None, 0, None
+        import torch
+        if stream is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        else:
+            with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(stream)):
+                workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+
+
+def quantize_rows(x, codes, scales, gate=None, stream=None):
+    """codes [n, code_ld(width)], scales [n, scale_ld(width)] of the rows of x (of x where gate > 0)."""
+    dt, (n, w) = _dtype(x), tuple(x.shape)
+    _on_device(x, codes, scales, gate)
+    px, ldx = _matrix(x, (n, w), x.dtype, "x")
+    pg, ldg = _matrix(gate, (n, w), x.dtype, "gate")
+    pc, ps = _code_rows(codes, scales, n, w, n, "codes")
+    _check(lib().varco_quantize_rows(dt, n, w, px, ldx, pg, ldg, pc, ps, _stream(stream)))
+
+
+def quantize_weights(h, turned=None, turned_scales=None, codes=None, scales=None, stream=None):
+    """Codes of fp32 weights h [n_in, n_out]: turned [n_out, code_ld(n_in)] for the forward product, codes [n_in, code_ld(n_out)] for
+    the input gradient; their scales have a row for each 128 rows of codes."""
+    import torch
+    n_in, n_out = tuple(h.shape)
+    _on_device(h, turned, turned_scales, codes, scales)
+    ph, ldh = _matrix(h, (n_in, n_out), torch.float32, "h")
+    pt, pts = _code_rows(turned, turned_scales, n_out, n_in, -(-n_out // CODE_BLOCK), "turned")
+    pc, ps = _code_rows(codes, scales, n_in, n_out, -(-n_in // CODE_BLOCK), "codes")
+    _check(lib().varco_quantize_weights(n_in, n_out, ph, ldh, pt, pts, pc, ps, _stream(stream)))
+
+
+def scaled_transform(codes, scales, w_codes, w_scales, n_in, c, accumulate=False, act=ACT_IDENTITY, stream=None):
+    """c = act((c +) X W): X rows of n_in codes, W the weights whose rows of codes are c's columns."""
+    dt, (n, n_out) = _dtype(c), tuple(c.shape)
+    _on_device(codes, scales, w_codes, w_scales, c)
+    pc, ldc = _matrix(c, (n, n_out), c.dtype, "c")
+    px, pxs = _code_rows(codes, scales, n, n_in, n, "codes")
+    pw, pws = _code_rows(w_codes, w_scales, n_out, n_in, -(-n_out // CODE_BLOCK), "w_codes")
+    _check(lib().varco_scaled_transform(dt, n, n_in, n_out, px, pxs, pw, pws, pc, ldc, int(accumulate), act, _stream(stream)))
+
+
+def scaled_weight_workspace(n_rows, n_in, n_out) -> int:
+    out = C.c_int64()
+    _check(lib().varco_scaled_weight_workspace(n_rows, n_in, n_out, C.byref(out)))
+    return out.value
+
+
+def scaled_bwd_weight(y_codes, y_scales, d_codes, d_scales, dh, accumulate=False, workspace=None, stream=None):
+    """dh (+)= Y^T D, dh [n_in, n_out] fp32, from rows of codes of the inputs and of the errors."""
+    import torch
+    n, (n_in, n_out) = y_codes.shape[0], tuple(dh.shape)
+    _on_device(y_codes, y_scales, d_codes, d_scales, dh, workspace)
+    ph, ldh = _matrix(dh, (n_in, n_out), torch.float32, "dh")
+    py, pys = _code_rows(y_codes, y_scales, n, n_in, n, "y_codes")
+    pd, pds = _code_rows(d_codes, d_scales, n, n_out, n, "d_codes")
+    pw, size, held = _scratch(scaled_weight_workspace(n, n_in, n_out) if workspace is None else 0, workspace, dh.device, stream)
+    _check(lib().varco_scaled_bwd_weight(n, n_in, n_out, py, pys, pd, pds, ph, ldh, int(accumulate), pw, size, _stream(stream)))
+
+
+def rms_norm_fwd(x, gain, eps, residual=None, total=None, y=None, codes=None, scales=None, inv_rms=None, stream=None):
+    """u = x + residual, y = u gain / sqrt(mean u^2 + eps); writes what is given of total (u), y, codes with scales, inv_rms."""
+    dt, (n, w) = _dtype(x), tuple(x.shape)
+    _on_device(x, gain, residual, total, y, codes, scales, inv_rms)
+    px, ldx = _matrix(x, (n, w), x.dtype, "x")
+    pr, ldr = _matrix(residual, (n, w), x.dtype, "residual")
+    pt, ldt = _matrix(total, (n, w), x.dtype, "total")
+    py, ldy = _matrix(y, (n, w), x.dtype, "y")
+    pc, ps = _code_rows(codes, scales, n, w, n, "codes")
+    _check(lib().varco_rms_norm_fwd(dt, n, w, px, ldx, pr, ldr, _vector(gain, w, "gain"), eps, pt, ldt, py, ldy, pc, ps,
+                                    _vector(inv_rms, n, "inv_rms"), _stream(stream)))
+
+
+def rms_norm_workspace(dtype, n_rows, width) -> int:
+    out = C.c_int64()
+    _check(lib().varco_rms_norm_workspace(dtype, n_rows, width, C.byref(out)))
+    return out.value
+
+
+def rms_norm_bwd(dy, u, gain, inv_rms, dx=None, dgain=None, dtotal=None, accumulate=False, workspace=None, stream=None):
+    """dx = gradient of u through the norm (+ dtotal); dgain (+)= the gain's gradient."""
+    dt, (n, w) = _dtype(dy), tuple(dy.shape)
+    _on_device(dy, u, gain, inv_rms, dx, dgain, dtotal, workspace)
+    pd, ldd = _matrix(dy, (n, w), dy.dtype, "dy")
+    pu, ldu = _matrix(u, (n, w), dy.dtype, "u")
+    pt, ldt = _matrix(dtotal, (n, w), dy.dtype, "dtotal")
+    px, ldx = _matrix(dx, (n, w), dy.dtype, "dx")
+    pw, size, held = _scratch(rms_norm_workspace(dt, n, w) if workspace is None and dgain is not None else 0, workspace, dy.device, stream)
+    _check(lib().varco_rms_norm_bwd(dt, n, w, pd, ldd, pu, ldu, _vector(gain, w, "gain"), _vector(inv_rms, n, "inv_rms"), pt, ldt, px, ldx,
+                                    _vector(dgain, w, "dgain"), int(accumulate), pw, size, _stream(stream)))
+
+
+class TensorList:
+    """Addresses and sizes of tensors that a program updates together, made once: device tensors of one type, each consecutive in
+    memory, none overlapping another. Holds the tensors."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        self.dtype = _dtype(self.tensors[0]) if self.tensors else F32
+        for t in self.tensors:
+            if _dtype(t) != self.dtype:
+                _refuse(ERR_UNSUPPORTED, "tensors of different types")
+            if not t.is_contiguous():
+                _refuse(ERR_SHAPE, "a tensor that is not consecutive in memory")
+            if t.get_device() != self.tensors[0].get_device() or not t.is_cuda:
+                _refuse(ERR_INVALID_ARG, "tensors on different devices or not on one")
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in self.tensors if t.numel())
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            _refuse(ERR_INVALID_ARG, "tensors that overlap")
+        n = len(self.tensors)
+        self.pointers = (C.c_void_p * n)(*[t.data_ptr() for t in self.tensors])
+        self.sizes = (C.c_int64 * n)(*[t.numel() for t in self.tensors])
+        self.need = gradient_norm_workspace(self)
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def _listed(tensors):
+    return tensors if isinstance(tensors, TensorList) else TensorList(tensors)
+
+
+def gradient_norm_workspace(tensors) -> int:
+    out = C.c_int64()
+    _check(lib().varco_gradient_norm_workspace(len(tensors), tensors.sizes, C.byref(out)))
+    return out.value
+
+
+def _same_sizes(a, b):
+    if len(a) != len(b) or a.dtype != b.dtype or bytes(a.sizes) != bytes(b.sizes):
+        _refuse(ERR_SHAPE, "lists of tensors that do not match")
+
+
+def _limit_out(out):
+    import torch
+    if out is None or out.dtype != torch.float32 or out.numel() != 2 or not out.is_contiguous():
+        _refuse(ERR_SHAPE, "out: 2 consecutive float32 values are needed")
+    return out.data_ptr()
+
+
+def gradient_norm(grads, max_norm, out, workspace=None, stream=None):
+    """out[0] = norm of all tensors of `grads` together, out[1] = min(1, max_norm / norm)."""
+    g = _listed(grads)
+    _on_device(out, workspace, *g.tensors[:1])
+    pw, size, held = _scratch(g.need, workspace, out.device, stream)
+    _check(lib().varco_gradient_norm(g.dtype, len(g), g.pointers, g.sizes, max_norm, _limit_out(out), pw, size, _stream(stream)))
+
+
+def clip_gradients(grads, max_norm, out, into=None, workspace=None, stream=None):
+    """gradient_norm, and into[t] = out[1] * grads[t] (into None: in place)."""
+    g = _listed(grads)
+    to = g if into is None else _listed(into)
+    _same_sizes(g, to)
+    _on_device(out, workspace, *g.tensors[:1], *to.tensors[:1])
+    pw, size, held = _scratch(g.need, workspace, out.device, stream)
+    _check(lib().varco_clip_gradients(g.dtype, len(g), g.pointers, to.pointers, g.sizes, max_norm, _limit_out(out), pw, size, _stream(stream)))
+
+
+def sgd_step_clipped(w, dw, lr, max_norm, out, workspace=None, stream=None):
+    """gradient_norm of dw, and w[t] -= lr * out[1] * dw[t] (fp32)."""
+    g, to = _listed(dw), _listed(w)
+    _same_sizes(g, to)
+    if g.dtype != F32:
+        _refuse(ERR_UNSUPPORTED, "weights and their gradients are float32")
+    _on_device(out, workspace, *g.tensors[:1], *to.tensors[:1])
+    pw, size, held = _scratch(g.need, workspace, out.device, stream)
+    _check(lib().varco_sgd_step_clipped(len(g), to.pointers, g.pointers, g.sizes, lr, max_norm, _limit_out(out), pw, size, _stream(stream)))
 
 
 # ---------------------------------------------------------------------------------------------------------

@@ -1,0 +1,124 @@
+// Rows of 8-bit codes: numbers of 4 exponent and 3 fraction bits (e4m3: no infinity, one NaN, largest 448), and a power of
+// two for each 128 columns of a row as their scale, stored as its exponent + 127 in a byte. A power of two costs no bits
+// of a floating number inside its range, and it is the form of scale that the matrix units apply by themselves.
+#pragma once
+
+#include "elem.h"
+
+constexpr int kCodeBlock = 128;                        // columns (of weights: rows and columns) of a scale
+constexpr int kOneScale = 127;                         // the byte of scale 1
+inline __host__ __device__ int64_t code_ld(int64_t width) { return (width + 15) / 16 * 16; }        // VARCO_CODE_LD
+inline __host__ __device__ int64_t scale_ld(int64_t width) { return (width + 511) / 512 * 4; }      // VARCO_SCALE_LD
+
+// Smallest e with a 2^-e <= 448 = 1.75 2^8, at least -127, for finite a >= 0; 0 for a = 0. (Numbers below 2^-126 have a
+// zero exponent field: the limit is theirs whatever it says.)
+__device__ __forceinline__ int code_exponent(float a) {
+    const int bits = int(__float_as_uint(a));
+    const int e = (bits >> 23) - 127 - 8 + ((bits & 0x7FFFFF) > 0x600000 ? 1 : 0);
+    return bits == 0 ? 0 : max(e, -127);
+}
+// 2^-e for -127 <= e <= 126.
+__device__ __forceinline__ float code_inverse(int e) { return __uint_as_float(uint32_t(127 - e) << 23); }
+
+__device__ __forceinline__ bool is_finite(float x) { return fabsf(x) < INFINITY; }
+// |x|, 0 for what is not finite: one such element does not take the other 127 of its block along.
+__device__ __forceinline__ float finite_size(float x) { return is_finite(x) ? fabsf(x) : 0.f; }
+
+// Four codes of values that `inverse` brings to 448 at most; infinities and NaN become the code of NaN.
+__device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float d, float inverse) {
+    auto in = [inverse](float x) { return is_finite(x) ? x * inverse : __uint_as_float(0x7FC00000u); };
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(in(a), in(b), 0, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(in(c), in(d), w, true);
+    return uint32_t(w);
+}
+
+// Lanes of a wavefront combined by data paths of the vector ALU: every lane gets the result over its group of N lanes
+// (N = 1, 2, 4, .., 64, groups aligned), the same bits in all of them.
+template <int CTRL>
+__device__ __forceinline__ float other_lane(float x) {
+    const int u = int(__float_as_uint(x));
+    return __uint_as_float(uint32_t(__builtin_amdgcn_update_dpp(u, u, CTRL, 0xF, 0xF, false)));
+}
+template <int N, typename F>
+__device__ __forceinline__ float over_lanes(float x, F f) {
+    if (N >= 2) x = f(x, other_lane<0xB1>(x));          // quad_perm 1 0 3 2
+    if (N >= 4) x = f(x, other_lane<0x4E>(x));          // quad_perm 2 3 0 1
+    if (N >= 8) x = f(x, other_lane<0x141>(x));         // row_half_mirror: the other four lanes of eight
+    if (N >= 16) x = f(x, other_lane<0x140>(x));        // row_mirror: the other eight of sixteen
+    if (N >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    if (N >= 64) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    return x;
+}
+template <int N>
+__device__ __forceinline__ float lanes_sum(float x) {
+    return over_lanes<N>(x, [](float a, float b) { return a + b; });
+}
+template <int N>
+__device__ __forceinline__ float lanes_max(float x) {
+    return over_lanes<N>(x, [](float a, float b) { return fmaxf(a, b); });
+}
+
+// A row in pieces of 16 bytes of its storage type, converted to fp32: any address of an element, any length.
+template <typename T>
+struct RowPiece {
+    static constexpr int P = 16 / int(sizeof(T));
+    static __device__ __forceinline__ void load(const T* row, int32_t at, int32_t width, float (&v)[P]) {
+        if (at + P <= width) {
+            if constexpr (sizeof(T) == 2) {
+                const uint4 u = load8_any(reinterpret_cast<const char*>(row + at));
+                const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+            } else {
+                typedef float any4 __attribute__((ext_vector_type(4), aligned(4)));
+                const any4 u = *reinterpret_cast<const any4*>(row + at);
+#pragma unroll
+                for (int i = 0; i < P; ++i) v[i] = u[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < P; ++i) v[i] = at + i < width ? Elem<T>::load(row + at + i) : 0.f;
+        }
+    }
+    static __device__ __forceinline__ void store(T* row, int32_t at, int32_t width, const float (&v)[P]) {
+        if (at + P <= width) {
+            if constexpr (sizeof(T) == 2) {
+                typedef uint32_t any4 __attribute__((ext_vector_type(4), aligned(2)));
+                any4 u;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) u[i] = bf16_pair(v[2 * i], v[2 * i + 1]);
+                *reinterpret_cast<any4*>(row + at) = u;
+            } else {
+                typedef float any4 __attribute__((ext_vector_type(4), aligned(4)));
+                any4 u;
+#pragma unroll
+                for (int i = 0; i < P; ++i) u[i] = v[i];
+                *reinterpret_cast<any4*>(row + at) = u;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < P; ++i)
+                if (at + i < width) Elem<T>::store(row + at + i, v[i]);
+        }
+    }
+    // The value that a stored element holds.
+    static __device__ __forceinline__ float rounded(float v) {
+        if constexpr (sizeof(T) == 2)
+            return bf16_to_float(float_to_bf16(v));
+        else
+            return v;
+    }
+    // This piece's codes, to `row` of code_ld(width) bytes.
+    static __device__ __forceinline__ void store_codes(uint8_t* row, int32_t at, const float (&v)[P], float inverse) {
+        if constexpr (P == 8)
+            *reinterpret_cast<uint2*>(row + at) = make_uint2(four_codes(v[0], v[1], v[2], v[3], inverse), four_codes(v[4], v[5], v[6], v[7], inverse));
+        else
+            *reinterpret_cast<uint32_t*>(row + at) = four_codes(v[0], v[1], v[2], v[3], inverse);
+    }
+};

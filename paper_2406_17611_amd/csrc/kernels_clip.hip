@@ -1,0 +1,222 @@
+// The norm of all gradients together, and gradients limited to it: out = f g or w -= lr f g with f = min(1, limit / norm).
+// Squares are summed in fp64 (a square of an fp32 number is exact there and neither overflows nor vanishes, and 300 million of them keep
+// 1e-13): the multiprocessors have that to spare, the kernels are bound by reading the gradients.
+// Two launches per 128 tensors: sums of squares per workgroup, then each workgroup of the second launch adds those few
+// sums itself, in one order, instead of a third launch that does it once.
+#include <algorithm>
+
+#include "codes_device.h"
+#include "varco_scaled.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTensors = 128;        // of one launch: their table is a kernel argument (4 KiB at most)
+constexpr int kMostPartials = 1024;  // sums of squares over all launches, but for one per launch more
+
+// Tensors are cut into chunks, numbered through the tensors of a launch.
+struct Table {
+    const void* src[kTensors];
+    int64_t n[kTensors];
+    int32_t first[kTensors + 1];
+    int32_t tensors, chunk;          // elements of a chunk: a multiple of 1024
+};
+struct OutTable {
+    const void* src[kTensors];
+    void* dst[kTensors];
+    int64_t n[kTensors];
+    int32_t first[kTensors + 1];
+    int32_t tensors, chunk;
+};
+static_assert(sizeof(OutTable) + 64 <= 4096, "a kernel's arguments");
+
+// The tensor that chunk c belongs to.
+template <typename TABLE>
+__device__ __forceinline__ int tensor_of(const TABLE& t, int32_t c) {
+    int lo = 0, hi = t.tensors - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (t.first[mid] <= c)
+            lo = mid;
+        else
+            hi = mid - 1;
+    }
+    return lo;
+}
+
+// Sum over the workgroup, in one order, in all its threads.
+__device__ __forceinline__ double block_sum(double x) {
+    __shared__ double part[kThreads];
+    __syncthreads();
+    part[threadIdx.x] = x;
+    __syncthreads();
+    for (int s = kThreads / 2; s > 0; s >>= 1) {
+        if (int(threadIdx.x) < s) part[threadIdx.x] += part[threadIdx.x + s];
+        __syncthreads();
+    }
+    return part[0];
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void square_sums_kernel(Table t, double* partial) {
+    using Row = RowPiece<T>;
+    constexpr int P = Row::P;
+    double sum[4] = {0.0, 0.0, 0.0, 0.0};
+    const int32_t chunks = t.first[t.tensors];
+    for (int32_t c = blockIdx.x; c < chunks; c += int32_t(gridDim.x)) {
+        const int k = tensor_of(t, c);
+        const int64_t at = int64_t(c - t.first[k]) * t.chunk;
+        const T* const p = static_cast<const T*>(t.src[k]) + at;
+        const int32_t n = int32_t(min(int64_t(t.chunk), t.n[k] - at));
+#pragma unroll 4
+        for (int32_t i = threadIdx.x * P; i < n; i += kThreads * P) {
+            float v[P];
+            Row::load(p, i, n, v);
+#pragma unroll
+            for (int j = 0; j < P; ++j) sum[j & 3] = fma(double(v[j]), double(v[j]), sum[j & 3]);
+        }
+    }
+    const double total = block_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
+    if (threadIdx.x == 0) partial[blockIdx.x] = total;
+}
+
+// Norm and factor from the sums of squares. A NaN or infinite norm is not below any limit: the factor becomes NaN or 0, and the
+// elements at fault stay visible.
+__device__ __forceinline__ float factor_of(const double* partial, int32_t n_partial, float max_norm, float* out) {
+    double x = 0.0;
+    for (int32_t i = threadIdx.x; i < n_partial; i += kThreads) x += partial[i];
+    const double norm = sqrt(block_sum(x));
+    const float f = norm <= double(max_norm) ? 1.f : float(double(max_norm) / norm);
+    if (out && threadIdx.x == 0) out[0] = float(norm), out[1] = f;
+    return f;
+}
+__global__ __launch_bounds__(kThreads) void norm_out_kernel(const double* partial, int32_t n_partial, float max_norm, float* out) {
+    factor_of(partial, n_partial, max_norm, out);
+}
+
+// STEP: dst -= lr f src (fp32), else dst = f src.
+template <typename T, bool STEP>
+__global__ __launch_bounds__(kThreads) void scale_kernel(OutTable t, const double* partial, int32_t n_partial, float max_norm, float lr, float* out) {
+    using Row = RowPiece<T>;
+    constexpr int P = Row::P;
+    float f = factor_of(partial, n_partial, max_norm, blockIdx.x == 0 ? out : nullptr);
+    const bool same = f == 1.f;
+    if (STEP) f *= lr;
+    const int32_t chunks = t.first[t.tensors];
+    for (int32_t c = blockIdx.x; c < chunks; c += int32_t(gridDim.x)) {
+        const int k = tensor_of(t, c);
+        const int64_t at = int64_t(c - t.first[k]) * t.chunk;
+        const T* const p = static_cast<const T*>(t.src[k]) + at;
+        T* const q = static_cast<T*>(t.dst[k]) + at;
+        if (!STEP && same && p == q) continue;             // in place and within the limit: the elements stay as they are
+        const int32_t n = int32_t(min(int64_t(t.chunk), t.n[k] - at));
+#pragma unroll 4
+        for (int32_t i = threadIdx.x * P; i < n; i += kThreads * P) {
+            float v[P], w[P];
+            Row::load(p, i, n, v);
+            if (STEP) Row::load(q, i, n, w);
+#pragma unroll
+            for (int j = 0; j < P; ++j) v[j] = STEP ? fmaf(-f, v[j], w[j]) : f * v[j];
+            Row::store(q, i, n, v);
+        }
+    }
+}
+
+int64_t total_of(int32_t n_tensors, const int64_t* sizes) {
+    int64_t n = 0;
+    for (int32_t i = 0; i < n_tensors; ++i) n += sizes[i];
+    return n;
+}
+// 1024 elements, up to 16 times as many where that still makes 2,048 chunks.
+int32_t chunk_of(int64_t total) { return int32_t(1024 * std::max<int64_t>(1, std::min<int64_t>(16, total / (1024 * 2048)))); }
+int64_t chunks_of(int64_t n, int64_t chunk) { return (n + chunk - 1) / chunk; }
+
+// Calls f(first tensor, tensors, chunks before, chunks) for each launch.
+template <typename F>
+void over_launches(int32_t n_tensors, const int64_t* sizes, int64_t chunk, F f) {
+    for (int32_t i = 0; i < n_tensors; i += kTensors) {
+        const int32_t n = std::min(kTensors, n_tensors - i);
+        int64_t chunks = 0;
+        for (int32_t k = 0; k < n; ++k) chunks += chunks_of(sizes[i + k], chunk);
+        if (chunks) f(i, n, chunks);
+    }
+}
+// Workgroups of a launch of the first kernel: its share of kMostPartials by its share of the elements, rounded up.
+int64_t workgroups(int64_t chunks, int64_t all) { return std::max<int64_t>(1, std::min(chunks, (kMostPartials * chunks + all - 1) / all)); }
+int64_t all_chunks(int32_t n_tensors, const int64_t* sizes, int64_t chunk) {
+    int64_t all = 0;
+    for (int32_t i = 0; i < n_tensors; ++i) all += chunks_of(sizes[i], chunk);
+    return all;
+}
+template <typename TABLE>
+void fill(TABLE& t, int32_t i, int32_t n, const void* const* src, const int64_t* sizes, int32_t chunk) {
+    int64_t c = 0;
+    for (int32_t k = 0; k < n; ++k) {
+        t.src[k] = src[i + k], t.n[k] = sizes[i + k], t.first[k] = int32_t(c);
+        c += chunks_of(sizes[i + k], chunk);
+    }
+    t.first[n] = int32_t(c);
+    t.tensors = n, t.chunk = chunk;
+}
+
+template <typename T, bool STEP>
+hipError_t launch_scale(int32_t n_tensors, const void* const* src, void* const* dst, const int64_t* sizes, const double* partial, int32_t n_partial,
+                        float max_norm, float lr, float* out, hipStream_t stream) {
+    const int32_t chunk = chunk_of(total_of(n_tensors, sizes));
+    hipError_t err = hipSuccess;
+    over_launches(n_tensors, sizes, chunk, [&](int32_t i, int32_t n, int64_t chunks) {
+        OutTable t;
+        fill(t, i, n, src, sizes, chunk);
+        for (int32_t k = 0; k < n; ++k) t.dst[k] = dst[i + k];
+        hipLaunchKernelGGL((scale_kernel<T, STEP>), dim3(unsigned(std::min<int64_t>(chunks, 2048))), dim3(kThreads), 0, stream, t, partial, n_partial,
+                           max_norm, lr, out);
+        if (err == hipSuccess) err = hipGetLastError();
+        out = nullptr;
+    });
+    return err;
+}
+
+}  // namespace
+
+int32_t varco_clip_partials(int32_t n_tensors, const int64_t* sizes) {
+    const int32_t chunk = chunk_of(total_of(n_tensors, sizes));
+    const int64_t all = all_chunks(n_tensors, sizes, chunk);
+    int64_t n = 0;
+    over_launches(n_tensors, sizes, chunk, [&](int32_t, int32_t, int64_t chunks) { n += workgroups(chunks, all); });
+    return int32_t(n);
+}
+
+hipError_t varco_launch_square_sums(int dtype, int32_t n_tensors, const void* const* grads, const int64_t* sizes, double* partial,
+                                    hipStream_t stream) {
+    const int32_t chunk = chunk_of(total_of(n_tensors, sizes));
+    const int64_t all = all_chunks(n_tensors, sizes, chunk);
+    hipError_t err = hipSuccess;
+    over_launches(n_tensors, sizes, chunk, [&](int32_t i, int32_t n, int64_t chunks) {
+        Table t;
+        fill(t, i, n, grads, sizes, chunk);
+        const int64_t blocks = workgroups(chunks, all);
+        if (dtype == VARCO_BF16)
+            hipLaunchKernelGGL(square_sums_kernel<bf16_t>, dim3(unsigned(blocks)), dim3(kThreads), 0, stream, t, partial);
+        else
+            hipLaunchKernelGGL(square_sums_kernel<float>, dim3(unsigned(blocks)), dim3(kThreads), 0, stream, t, partial);
+        if (err == hipSuccess) err = hipGetLastError();
+        partial += blocks;
+    });
+    return err;
+}
+
+hipError_t varco_launch_norm_out(const double* partial, int32_t n_partial, float max_norm, float* out, hipStream_t stream) {
+    hipLaunchKernelGGL(norm_out_kernel, dim3(1), dim3(kThreads), 0, stream, partial, n_partial, max_norm, out);
+    return hipGetLastError();
+}
+
+hipError_t varco_launch_clip(int dtype, int32_t n_tensors, const void* const* grads, void* const* into, const int64_t* sizes,
+                             const double* partial, int32_t n_partial, float max_norm, float* out, hipStream_t stream) {
+    if (dtype == VARCO_BF16) return launch_scale<bf16_t, false>(n_tensors, grads, into, sizes, partial, n_partial, max_norm, 0.f, out, stream);
+    return launch_scale<float, false>(n_tensors, grads, into, sizes, partial, n_partial, max_norm, 0.f, out, stream);
+}
+
+hipError_t varco_launch_sgd_clipped(int32_t n_tensors, void* const* w, const void* const* dw, const int64_t* sizes, float lr,
+                                    const double* partial, int32_t n_partial, float max_norm, float* out, hipStream_t stream) {
+    return launch_scale<float, true>(n_tensors, dw, w, sizes, partial, n_partial, max_norm, lr, out, stream);
+}

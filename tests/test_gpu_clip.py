@@ -1,0 +1,117 @@
+"""The norm of many gradients and steps limited by it, through the C ABI, against fp64. The norm is summed in fp64 and rounded once; the
+factor is rounded once, a limited element once more."""
+import numpy as np
+import pytest
+import torch
+
+from codes_common import STEP, assert_within, f64
+from oracle import codes as oc
+from paper_2406_17611_amd import binding as vb
+
+pytestmark = pytest.mark.gpu
+
+F = 2.0 ** -24
+SETS = {
+    "one element": [1], "none": [], "empty ones": [0, 0], "network": [25600, 25600, 65536, 65536, 12032, 12032],
+    "ragged": [1, 2, 3, 1023, 1024, 1025, 0, 77, 40001], "many": [(i * 37) % 301 for i in range(400)], "long": [3_000_001, 5],
+}
+
+
+def _tensors(sizes, dtype, seed, scale=1.0):
+    """Views that start at any element of one buffer."""
+    g = torch.Generator().manual_seed(seed)
+    flat = (torch.randn(sum(sizes) + 2 * len(sizes) + 1, generator=g) * scale).to(dtype).cuda()
+    out, at = [], 1
+    for n in sizes:
+        out.append(flat[at:at + n])
+        at += n + 2
+    return out, flat
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("name", SETS)
+@pytest.mark.parametrize("share", [0.3, 2.0])
+def test_clip(dtype, name, share):
+    grads, flat = _tensors(SETS[name], dtype, 1)
+    into, other = _tensors(SETS[name], dtype, 2)
+    norm, _ = oc.limit([f64(g) for g in grads], 1.0)
+    limit = float(np.float32(norm * share + (share if norm == 0 else 0)))
+    want = oc.limit([f64(g) for g in grads], limit)
+    before, between = flat.clone(), other.clone()
+    out = torch.full((2,), float("nan"), device="cuda")
+    vb.gradient_norm(grads, limit, out)
+    assert_within(f64(out), want, 2 * F * np.abs(want), "norm and factor")
+    again = torch.empty_like(out)
+    vb.clip_gradients(grads, limit, again, into=into)
+    assert torch.equal(out, again) and torch.equal(flat, before)
+    for a, g in zip(into, grads):
+        assert_within(f64(a), want[1] * f64(g), (2 * F + STEP[dtype]) * np.abs(want[1] * f64(g)) + 1e-38, "into")
+        between_view = between[a.storage_offset():a.storage_offset() + a.numel()]
+        between_view.copy_(a)
+    assert torch.equal(other, between)                                 # nothing between the tensors was written
+    vb.clip_gradients(grads, limit, again)
+    for a, g in zip(into, grads):
+        assert torch.equal(a, g)
+
+
+@pytest.mark.parametrize("name", SETS)
+def test_step(name):
+    grads, _ = _tensors(SETS[name], torch.float32, 3)
+    weights, flat = _tensors(SETS[name], torch.float32, 4)
+    start = [f64(w) for w in weights]
+    limit = 0.5
+    want = oc.limit([f64(g) for g in grads], limit)
+    out = torch.empty(2, device="cuda")
+    vb.sgd_step_clipped(weights, grads, 0.1, limit, out)
+    assert_within(f64(out), want, 2 * F * np.abs(want), "norm and factor")
+    for w, s, g in zip(weights, start, grads):
+        d = np.float64(np.float32(0.1)) * want[1] * f64(g)
+        assert_within(f64(w), s - d, F * np.abs(s - d) + 5 * F * np.abs(d) + 1e-38, "w")
+
+
+def test_large_and_small_numbers_keep_their_norm():
+    """Squares that fp32 cannot hold."""
+    for scale in (2.0 ** 100, 2.0 ** -100):
+        g = [torch.full((1000,), 3.0 * scale, device="cuda"), torch.full((500,), -1.0 * scale, device="cuda")]
+        out = torch.empty(2, device="cuda")
+        vb.gradient_norm(g, 1.0, out)
+        want = oc.limit([f64(t) for t in g], 1.0)
+        assert_within(f64(out), want, 2 * F * np.abs(want), "norm")
+
+
+def test_not_finite():
+    g = [torch.ones(100, device="cuda"), torch.ones(3, device="cuda")]
+    out = torch.empty(2, device="cuda")
+    g[0][7] = float("inf")
+    vb.clip_gradients(g, 1.0, out)
+    assert float(out[0]) == float("inf") and float(out[1]) == 0.0
+    assert torch.isnan(g[0][7]) and int(torch.isnan(g[0]).sum()) == 1 and (g[1] == 0).all()
+    g[1][0] = float("nan")
+    vb.gradient_norm(g, 1.0, out)
+    assert torch.isnan(out).all()
+
+
+def test_limits_of_nothing_and_everything():
+    g = [torch.randn(50, device="cuda")]
+    keep = g[0].clone()
+    out = torch.empty(2, device="cuda")
+    vb.clip_gradients(g, float("inf"), out)
+    assert torch.equal(g[0], keep) and float(out[1]) == 1.0
+    vb.clip_gradients(g, 0.0, out)
+    assert (g[0] == 0).all() and float(out[1]) == 0.0
+    vb.clip_gradients(g, 0.0, out)
+    assert float(out[0]) == 0.0 and float(out[1]) == 1.0
+
+
+def test_lists_are_checked():
+    a = torch.zeros(10, device="cuda")
+    for bad in ([a, a], [a[:6], a[5:]], [a, torch.zeros(3)], [a, torch.zeros(3, dtype=torch.bfloat16, device="cuda")], [torch.zeros(4, 4, device="cuda").t()[1:]]):
+        with pytest.raises(vb.VarcoError):
+            vb.TensorList(bad)
+    out = torch.empty(2, device="cuda")
+    with pytest.raises(vb.VarcoError):
+        vb.clip_gradients([a], 1.0, out, into=[torch.zeros(9, device="cuda")])
+    with pytest.raises(vb.VarcoError):
+        vb.sgd_step_clipped([a.bfloat16()], [a.bfloat16()], 0.1, 1.0, out)
+    with pytest.raises(vb.VarcoError):
+        vb.gradient_norm([a], -1.0, out)

@@ -1,0 +1,159 @@
+"""Products of 8-bit codes, through the C ABI, against fp64 products of what the codes stand for. Bounds: sums of K exact products
+in fp32 are off by at most K 2^-24 of the sum of their sizes, whatever their order; a result is rounded once to its type. bf16 results come
+from the 8-bit units, which drop of each of eight consecutive products what lies below 2^-13 of the largest one's power of two."""
+import numpy as np
+import pytest
+import torch
+
+from codes_common import STEP, assert_within, f64, strided, upload_codes
+from oracle import codes as oc
+from paper_2406_17611_amd import binding as vb
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [torch.float32, torch.bfloat16]
+
+
+def _coded(n, w, seed):
+    rng = np.random.default_rng(seed)
+    v = rng.standard_normal((n, w)) * np.exp(rng.standard_normal((n, 1)) * 3)
+    if n > 2:
+        v[n // 2] = 0.0
+    return oc.quantize_rows(v)
+
+
+def _weights(n_in, n_out, seed):
+    rng = np.random.default_rng(seed)
+    h = rng.standard_normal((n_in, n_out)) * np.exp(rng.standard_normal((n_in, 1)))
+    codes, exps = oc.quantize_weights(h)
+    return oc.weight_values(codes, exps), upload_codes(codes.T, exps.T, n_in), upload_codes(codes, exps, n_out)
+
+
+def _dropped(dtype, x, w):
+    """What the sums behind an element of x w may lack besides the additions' roundings."""
+    if dtype == torch.float32:
+        return 0.0
+    out = np.zeros((x.shape[0], w.shape[1]))
+    for k in range(0, x.shape[1], 8):
+        p = np.abs(x[:, k:k + 8, None] * w[None, k:k + 8, :])
+        out += 8 * 2.0 ** -13 * p.max(axis=1)
+    return out
+
+
+SIZES = [(1, 1, 1), (1, 256, 47), (3, 128, 16), (129, 47, 256), (200, 100, 129), (257, 513, 40), (130, 300, 260), (64, 2048, 130),
+         (1000, 256, 256), (515, 640, 513), (33, 16384, 8), (17, 16, 4000)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,n_in,n_out", SIZES)
+def test_transform(dtype, n, n_in, n_out):
+    codes, exps = _coded(n, n_in, n + n_in)
+    w, turned, _ = _weights(n_in, n_out, n_out)
+    x = oc.values(codes, exps)
+    want, size = x @ w, np.abs(x) @ np.abs(w)
+    c = torch.full((n, n_out), float("nan"), dtype=dtype, device="cuda")
+    vb.scaled_transform(*upload_codes(codes, exps, n_in), *turned, n_in, c)
+    sums = n_in * 2.0 ** -24 * size + _dropped(dtype, x, w)
+    assert_within(f64(c), want, sums + STEP[dtype] * (np.abs(want) + sums) + 1e-38, "c")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,n_in,n_out", [(5, 128, 8), (131, 100, 47), (400, 260, 300)])
+@pytest.mark.parametrize("act", [vb.ACT_IDENTITY, vb.ACT_RELU])
+def test_added_to_rows_of_wider_memory(dtype, n, n_in, n_out, act):
+    codes, exps = _coded(n, n_in, 1)
+    w, turned, _ = _weights(n_in, n_out, 2)
+    x = oc.values(codes, exps)
+    start = torch.randn(n, n_out, generator=torch.Generator().manual_seed(3)).to(dtype).cuda()
+    c, flat = strided(start, 3, 1)
+    want, size = f64(start) + x @ w, np.abs(f64(start)) + np.abs(x) @ np.abs(w)
+    if act == vb.ACT_RELU:
+        want = np.maximum(want, 0.0)
+    vb.scaled_transform(*upload_codes(codes, exps, n_in), *turned, n_in, c, accumulate=True, act=act)
+    sums = (n_in + 1) * 2.0 ** -24 * size + _dropped(dtype, x, w)
+    assert_within(f64(c), want, sums + STEP[dtype] * (np.abs(want) + sums), "c")
+    behind = flat[1:].view(n, n_out + 3)[:, n_out:]
+    assert torch.isnan(behind).all() and torch.isnan(flat[0])          # what lies between the rows is left alone
+
+
+@pytest.mark.parametrize("n,n_in,n_out", [(77, 100, 47), (260, 256, 129)])
+def test_input_gradient_takes_the_other_copy(n, n_in, n_out):
+    codes, exps = _coded(n, n_out, 4)
+    w, _, plain = _weights(n_in, n_out, 5)
+    d = oc.values(codes, exps)
+    dx = torch.empty((n, n_in), device="cuda")
+    vb.scaled_transform(*upload_codes(codes, exps, n_out), *plain, n_out, dx)
+    assert_within(f64(dx), d @ w.T, (n_out + 1) * 2.0 ** -24 * (np.abs(d) @ np.abs(w.T)), "dx")
+
+
+def test_scales_from_one_end_to_the_other():
+    """Scales of a row's blocks 2^120 apart, and of the weights' against them."""
+    rng = np.random.default_rng(7)
+    n, n_in, n_out = 20, 384, 20
+    v = rng.standard_normal((n, n_in))
+    v[:, :128] *= 2.0 ** 60
+    v[:, 256:] *= 2.0 ** -60
+    h = rng.standard_normal((n_in, n_out))
+    h[:128] *= 2.0 ** -60
+    h[256:] *= 2.0 ** 60
+    codes, exps = oc.quantize_rows(v)
+    hc, he = oc.quantize_weights(h)
+    x, w = oc.values(codes, exps), oc.weight_values(hc, he)
+    c = torch.empty((n, n_out), device="cuda")
+    vb.scaled_transform(*upload_codes(codes, exps, n_in), *upload_codes(hc.T, he.T, n_in), n_in, c)
+    assert_within(f64(c), x @ w, n_in * 2.0 ** -24 * (np.abs(x) @ np.abs(w)), "c")
+
+
+def test_a_nan_code_reaches_its_row_only():
+    codes, exps = _coded(40, 200, 8)
+    codes[7, 150] = oc.NAN_CODE
+    w, turned, _ = _weights(200, 70, 9)
+    for act in (vb.ACT_IDENTITY, vb.ACT_RELU):
+        c = torch.empty((40, 70), device="cuda")
+        vb.scaled_transform(*upload_codes(codes, exps, 200), *turned, 200, c, act=act)
+        bad = torch.isnan(c).cpu().numpy()
+        assert bad[7].all() and not np.delete(bad, 7, axis=0).any()
+
+
+WEIGHTS = [(0, 16, 16), (1, 1, 1), (1, 128, 128), (31, 100, 47), (33, 256, 16), (1000, 130, 260), (2500, 47, 300), (4100, 300, 100),
+           (700, 1000, 40), (513, 2048, 130)]
+
+
+@pytest.mark.parametrize("n,n_in,n_out", WEIGHTS)
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_weight_gradient(n, n_in, n_out, accumulate):
+    yc, ye = _coded(n, n_in, 11) if n else (np.empty((0, n_in), np.uint8), np.empty((0, -(-n_in // 128)), np.int64))
+    dc, de = _coded(n, n_out, 12) if n else (np.empty((0, n_out), np.uint8), np.empty((0, -(-n_out // 128)), np.int64))
+    y, d = oc.values(yc, ye), oc.values(dc, de)
+    start = torch.randn(n_in, n_out, generator=torch.Generator().manual_seed(13)).cuda()
+    dh, flat = strided(start, 2, 1)
+    want, size = y.T @ d, np.abs(y.T) @ np.abs(d)
+    if accumulate:
+        want, size = want + f64(start), size + np.abs(f64(start))
+    vb.scaled_bwd_weight(*upload_codes(yc, ye, n_in), *upload_codes(dc, de, n_out), dh, accumulate=accumulate)
+    assert_within(f64(dh), want, (n + 1) * 2.0 ** -24 * size, "dh")
+    assert torch.isnan(flat[1:].view(n_in, n_out + 2)[:, n_out:]).all() and torch.isnan(flat[0])
+
+
+def test_every_code_and_scale_is_read_as_what_it_stands_for():
+    """One row per scale, all 254 codes that are numbers against a single 1: the conversion to the products' operands, exactly."""
+    codes = np.array([b for b in range(256) if b & 0x7F != 0x7F], dtype=np.uint8)
+    ones, zero = np.full((1, 1), 0x38, np.uint8), np.zeros((1, 1), np.int64)
+    for e in (-118, -60, -8, 0, 9, 60, 118):
+        yc, ye = codes[None, :], np.full((1, 2), e, np.int64)
+        dh = torch.empty((254, 1), device="cuda")
+        vb.scaled_bwd_weight(*upload_codes(yc, ye, 254), *upload_codes(ones, zero, 1), dh)
+        assert np.array_equal(f64(dh)[:, 0], oc.values(yc, ye)[0]), e
+        c = torch.empty((254, 1), device="cuda")
+        vb.scaled_transform(*upload_codes(codes[:, None], np.full((254, 1), e, np.int64), 1), *upload_codes(ones, zero, 1), 1, c)
+        assert np.array_equal(f64(c)[:, 0], oc.values(yc, ye)[0]), e
+
+
+def test_sums_are_the_same_every_time():
+    yc, ye = _coded(3000, 150, 14)
+    dc, de = _coded(3000, 90, 15)
+    y, d = upload_codes(yc, ye, 150), upload_codes(dc, de, 90)
+    out = [torch.empty((150, 90), device="cuda") for _ in range(3)]
+    for t in out:
+        vb.scaled_bwd_weight(*y, *d, t)
+    assert torch.equal(out[0], out[1]) and torch.equal(out[0], out[2])
