@@ -11,6 +11,7 @@
 // g + 4 of the 8 of a block, g = lane / 16, in both operands. (The order inside a block of 128 is free as long as both have the same.)
 // The weights are the first operand: a lane then holds four consecutive outputs of one row.
 #include <algorithm>
+#include <type_traits>
 
 #include "codes_device.h"
 #include "varco_scaled.h"
@@ -23,15 +24,17 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
-constexpr int kTile = 128;           // rows and outputs of a tile; a wavefront takes 64 x 64
 constexpr int BK = kCodeBlock;
 
-// 16-byte piece p of row r of a tile: 128 bytes per row, pieces moved so that eight rows read at one piece use all banks.
-__device__ __forceinline__ int piece_at(int r, int p) { return r * BK + ((p ^ (r & 7)) << 4); }
+// Two pieces of 16 bytes as a fragment of the 8-bit unit.
+__device__ __forceinline__ intx8 joined(const uint4& lo, const uint4& hi) {
+    return intx8{int(lo.x), int(lo.y), int(lo.z), int(lo.w), int(hi.x), int(hi.y), int(hi.z), int(hi.w)};
+}
 
 // A fragment's 32 codes as four fragments of the bf16 unit.
 struct Bf16Fragment {
     bf16x8 f[4];
+    Bf16Fragment() = default;
     __device__ __forceinline__ Bf16Fragment(const intx8& q, int scale) {
         const float x = __uint_as_float(scale ? uint32_t(scale) << 23 : 0x400000u);
 #pragma unroll
@@ -47,96 +50,328 @@ struct Bf16Fragment {
     }
 };
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void scaled_kernel(ScaledArgs a) {
-    __shared__ __attribute__((aligned(16))) uint8_t lx[kTile * BK];
-    __shared__ __attribute__((aligned(16))) uint8_t lw[kTile * BK];
-    const int64_t m0 = int64_t(blockIdx.x) * kTile;
-    const int32_t n0 = int32_t(blockIdx.y) * kTile;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, l = lane & 15;
-    const int wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
+// N consecutive outputs of a row, from column n on.
+template <typename T, int N>
+__device__ __forceinline__ void store_outputs(T* row, int32_t n, const ScaledArgs& a, const float (&v)[N]) {
+    constexpr int P = RowPiece<T>::P;
+#pragma unroll
+    for (int i = 0; i < N; i += P) {
+        float x[P];
+        if (a.accumulate) {
+            RowPiece<T>::load(row, n + i, a.n_out, x);
+#pragma unroll
+            for (int j = 0; j < P; ++j) x[j] += v[i + j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < P; ++j) x[j] = v[i + j];
+        }
+        if (a.relu)
+#pragma unroll
+            for (int j = 0; j < P; ++j) x[j] = x[j] < 0.f ? 0.f : x[j];         // (NaN stays)
+        RowPiece<T>::store(row, n + i, a.n_out, x);
+    }
+}
+
+// What the pieces behind the last column of a row are loaded from.
+__device__ __attribute__((aligned(16))) const uint8_t zero_piece[16] = {};
+
+// 16 bytes per lane from memory to LDS, lane after lane from `to` on, without a register between (waited for by vmcnt).
+__device__ __forceinline__ void copy_to_lds(const uint8_t* from, uint8_t* to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+// This thread's copies and LDS reads are done, then everybody's.
+__device__ __forceinline__ void copies_done() {
+    __builtin_amdgcn_s_waitcnt(0x0070);        // vmcnt(0) lgkmcnt(0)
+    __syncthreads();
+}
+
+// Order of a row's 16-byte pieces in LDS: the 16 rows that a fragment takes meet all eight places of a row's 128 bytes. Rows of X are
+// consecutive, those of W are the ones described at scaled_rows_kernel.
+__device__ __forceinline__ int place_x(int row) { return row & 7; }
+__device__ __forceinline__ int place_w(int row) { return (row & 3) | ((row >> 2) & 4); }
+
+// Long reductions: tiles of 16 MI WM rows x 64 WN outputs, a block of 128 of the reduction at a time through LDS, copied there while the
+// block before is multiplied (two buffers).
+template <typename T, int WM, int WN, int MI>
+__global__ __launch_bounds__(64 * WM * WN, 2) void scaled_tile_kernel(ScaledArgs a, int32_t tiles_n, int32_t tiles) {
+    constexpr int WAVES = WM * WN, BM = 16 * MI * WM, BN = 64 * WN, NX = BM / 8 / WAVES, NW = BN / 8 / WAVES;
+    static_assert(NX * 8 * WAVES == BM && NW * 8 * WAVES == BN, "every wavefront copies as many rows");
+    __shared__ __attribute__((aligned(16))) uint8_t x0[BM * BK], w0[BN * BK], x1[BM * BK], w1[BN * BK];       // (apart, so that copies to one pair are not taken to alias reads of the other)
+    // tiles are dealt to the 8 XCDs in runs, the tiles of the same rows one after the other: they share X in the L2 of their XCD
+    const int32_t run = (tiles + 7) / 8, tile = int32_t(blockIdx.x & 7) * run + int32_t(blockIdx.x >> 3);
+    if (int32_t(blockIdx.x >> 3) >= run || tile >= tiles) return;       // whole workgroup
+    const int64_t m0 = int64_t(tile / tiles_n) * BM;
+    const int32_t n0 = tile % tiles_n * BN;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, l = lane & 15;
+    const int wm = wave / WN * (16 * MI), wn = wave % WN * 64;
     const int64_t ld = code_ld(a.n_in), lds = scale_ld(a.n_in);
     const int32_t steps = (a.n_in + BK - 1) / BK;
-    floatx4 acc[4][4];
+    const int32_t tail = ld % BK == 0 ? BK : int32_t(ld % BK);         // bytes of the last block that there are
+
+    // what a lane copies: piece (lane % 8) of LDS row 8 h' + lane / 8, as bytes from the tile's first row
+    const uint8_t* const base_x = a.x + m0 * ld;
+    const uint8_t* const base_w = a.w + int64_t(n0) * ld;
+    const int last_m = int(min(int64_t(BM), a.n_rows - m0)) - 1, last_n = min(BN, a.n_out - n0) - 1;
+    const int sub = lane >> 3, piece_x = 16 * ((lane & 7) ^ sub);
+    uint32_t at_x[NX], at_w[NW];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int h = 0; h < NX; ++h) at_x[h] = uint32_t(min((wave * NX + h) * 8 + sub, last_m)) * uint32_t(ld) + piece_x;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = floatx4(0.f);
-    for (int32_t s = 0; s < steps; ++s) {
-        uint4 vx[4], vw[4];
+    for (int h = 0; h < NW; ++h) {
+        const int r = (wave * NW + h) * 8 + sub;
+        at_w[h] = uint32_t(min(r, last_n)) * uint32_t(ld) + 16 * ((lane & 7) ^ place_w(r));
+    }
+    auto copy = [&](int32_t s, uint8_t* lx, uint8_t* lw) {
+        const uint8_t* const x = base_x + int64_t(s) * BK;
+        const uint8_t* const w = base_w + int64_t(s) * BK;
+        if (s + 1 < steps || tail == BK) {
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
-            const int e = threadIdx.x + h * kThreads, r = e >> 3, p = e & 7;
-            const int64_t k = int64_t(s) * BK + p * 16;
-            vx[h] = vw[h] = make_uint4(0u, 0u, 0u, 0u);
-            if (k < ld && m0 + r < a.n_rows) vx[h] = *reinterpret_cast<const uint4*>(a.x + (m0 + r) * ld + k);
-            if (k < ld && n0 + r < a.n_out) vw[h] = *reinterpret_cast<const uint4*>(a.w + (n0 + r) * ld + k);
+            for (int h = 0; h < NX; ++h) copy_to_lds(x + at_x[h], lx + (wave * NX + h) * 1024);
+#pragma unroll
+            for (int h = 0; h < NW; ++h) copy_to_lds(w + at_w[h], lw + (wave * NW + h) * 1024);
+        } else {
+#pragma unroll
+            for (int h = 0; h < NX; ++h) copy_to_lds(piece_x < tail ? x + at_x[h] : zero_piece, lx + (wave * NX + h) * 1024);
+#pragma unroll
+            for (int h = 0; h < NW; ++h)
+                copy_to_lds(16 * ((lane & 7) ^ place_w((wave * NW + h) * 8 + sub)) < tail ? w + at_w[h] : zero_piece, lw + (wave * NW + h) * 1024);
         }
-        __syncthreads();
+    };
+    // the scales of four blocks at a time
+    const uint8_t* const base_sx = a.x_scales + m0 * lds;
+    const int* const from_sw = reinterpret_cast<const int*>(a.w_scales + int64_t(min(n0 + wn, a.n_out - 1) / kCodeBlock) * lds);
+    int sx[MI], next_sx[MI], sw = 0;
+    auto scales = [&](int32_t s) {
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
-            const int e = threadIdx.x + h * kThreads, r = e >> 3, p = e & 7;
-            *reinterpret_cast<uint4*>(lx + piece_at(r, p)) = vx[h];
-            *reinterpret_cast<uint4*>(lw + piece_at(r, p)) = vw[h];
-        }
-        __syncthreads();
-        const int scale_w = a.w_scales[(n0 / kCodeBlock) * lds + s];
-        auto fragment = [&](const uint8_t* t, int r) {
-            const uint4 lo = *reinterpret_cast<const uint4*>(t + piece_at(r + l, g)), hi = *reinterpret_cast<const uint4*>(t + piece_at(r + l, g + 4));
-            return intx8{int(lo.x), int(lo.y), int(lo.z), int(lo.w), int(hi.x), int(hi.y), int(hi.z), int(hi.w)};
-        };
+        for (int j = 0; j < MI; ++j) next_sx[j] = *reinterpret_cast<const int*>(base_sx + s + uint32_t(min(wm + 16 * j + l, last_m)) * uint32_t(lds));
+    };
+
+    floatx4 acc[MI][4];
+#pragma unroll
+    for (int j = 0; j < MI; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[j][i] = floatx4(0.f);
+    auto fragment = [&](const uint8_t* t, int r, int place) {
+        return joined(*reinterpret_cast<const uint4*>(t + r * BK + ((g ^ place) << 4)), *reinterpret_cast<const uint4*>(t + r * BK + (((g + 4) ^ place) << 4)));
+    };
+    const int row_w = wn + (l >> 2) * 16 + (l & 3);
+    auto multiply = [&](const uint8_t* lx, const uint8_t* lw) {
         if constexpr (sizeof(T) == 2) {
             intx8 fw[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) fw[i] = fragment(lw, wn + 16 * i);
+            for (int i = 0; i < 4; ++i) fw[i] = fragment(lw, row_w + 4 * i, place_w(row_w + 4 * i));
+            intx8 fx = fragment(lx, wm + l, place_x(l));
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const intx8 fx = fragment(lx, wm + 16 * j);
-                const int scale_x = a.x_scales[min(m0 + wm + 16 * j + l, a.n_rows - 1) * lds + s];
+            for (int j = 0; j < MI; ++j) {
+                intx8 next = fx;
+                if (j + 1 < MI) next = fragment(lx, wm + 16 * (j + 1) + l, place_x(l));
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[i], fx, acc[i][j], 0, 0, 0, scale_w, 0, scale_x);
+                for (int i = 0; i < 4; ++i) acc[j][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[i], fx, acc[j][i], 0, 0, 0, sw, 0, sx[j]);
+                fx = next;
+                __builtin_amdgcn_sched_barrier(0);         // (one fragment ahead: all of them at once do not fit the registers)
             }
         } else {
+            Bf16Fragment fw[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const Bf16Fragment fx(fragment(lx, wm + 16 * j), a.x_scales[min(m0 + wm + 16 * j + l, a.n_rows - 1) * lds + s]);
+            for (int i = 0; i < 4; ++i) fw[i] = Bf16Fragment(fragment(lw, row_w + 4 * i, place_w(row_w + 4 * i)), sw & 255);
+            intx8 fx = fragment(lx, wm + l, place_x(l));
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const Bf16Fragment fw(fragment(lw, wn + 16 * i), scale_w);
+            for (int j = 0; j < MI; ++j) {
+                const Bf16Fragment x(fx, sx[j] & 255);
+                if (j + 1 < MI) fx = fragment(lx, wm + 16 * (j + 1) + l, place_x(l));
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw.f[q], fx.f[q], acc[i][j], 0, 0, 0);
-                }
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[i].f[q], x.f[q], acc[j][i], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
-    }
-    // accumulator v of a lane: output 4 (lane / 16) + v, row lane % 16
+    };
+    auto block = [&](int32_t s, const uint8_t* lx, const uint8_t* lw, uint8_t* next_x, uint8_t* next_w) {
+        copies_done();
+        if ((s & 3) == 0) {
+            sw = from_sw[s >> 2];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < MI; ++j) sx[j] = next_sx[j];
+        } else {
+            sw = int(uint32_t(sw) >> 8);
+#pragma unroll
+            for (int j = 0; j < MI; ++j) sx[j] = int(uint32_t(sx[j]) >> 8);
+        }
+        if (s + 1 < steps) {
+            if ((s & 3) == 3) scales(s + 1);
+            copy(s + 1, next_x, next_w);
+        }
+        multiply(lx, lw);
+    };
+    scales(0);
+    copy(0, x0, w0);
+    for (int32_t s = 0; s < steps; s += 2) {
+        block(s, x0, w0, x1, w1);
+        if (s + 1 < steps) block(s + 1, x1, w1, x0, w0);
+    }
+#pragma unroll
+    for (int j = 0; j < MI; ++j) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(acc[j][i]));
         const int64_t row = m0 + wm + 16 * j + l;
         if (row >= a.n_rows) continue;
-        T* const c = static_cast<T*>(a.c) + row * a.ldc;
+        float v[16];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const int32_t n = n0 + wn + 16 * i + 4 * g + v;
-                if (n >= a.n_out) continue;
-                float x = acc[i][j][v];
-                if (a.accumulate) x += Elem<T>::load(c + n);
-                if (a.relu) x = x < 0.f ? 0.f : x;         // (NaN stays)
-                Elem<T>::store(c + n, x);
+            for (int q = 0; q < 4; ++q) v[4 * i + q] = acc[j][i][q];
+        store_outputs(static_cast<T*>(a.c) + row * a.ldc, n0 + wn + 16 * g, a, v);
+    }
+}
+
+// Short reductions (512 at most): bound by reading X and writing c. A wavefront keeps the weights of 16 NI outputs in registers
+// and walks over rows, 16 R at a time, the next ones requested before the present ones are multiplied; nothing passes through LDS.
+// WN wavefronts of a workgroup take the same rows (their other outputs), which the second to fourth find in the caches.
+// Weight row 4 NI (a / 4) + 4 i + a % 4 of them is row a of fragment i: accumulators 0 .. 3 of the NI fragments are then consecutive
+// outputs of a lane's row, up to 64 bytes to store.
+// NI: 4; 2 where fp32 results take more than 256 columns, whose weights are kept as bf16 (twice the registers).
+// (The empty assembly keeps the products in front of the stores' branches: under a branch the lanes that do not take it would
+// supply nothing to the matrix instruction.)
+template <typename T, int KB, int NI, int WN, int R>
+__global__ __launch_bounds__(kThreads, 2) void scaled_rows_kernel(ScaledArgs a) {
+    constexpr int WR = kThreads / 64 / WN;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, l = lane & 15;
+    const int32_t n0 = (int32_t(blockIdx.y) * WN + wave % WN) * (16 * NI);
+    if (n0 >= a.n_out) return;                         // (no barriers here)
+    const uint32_t ld = uint32_t(code_ld(a.n_in));
+    auto load = [&](const uint8_t* row, int kb) {
+        const uint32_t k = kb * kCodeBlock + g * 16;
+        uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo;
+        if (k < ld) lo = *reinterpret_cast<const uint4*>(row + k);
+        if (k + 64 < ld) hi = *reinterpret_cast<const uint4*>(row + k + 64);
+        return joined(lo, hi);
+    };
+    intx8 fw[NI][KB];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+        const uint8_t* const row = a.w + int64_t(min(n0 + (l >> 2) * (4 * NI) + 4 * i + (l & 3), a.n_out - 1)) * ld;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) fw[i][kb] = load(row, kb);
+    }
+    const int scale_w = *reinterpret_cast<const int*>(a.w_scales + int64_t(n0 / kCodeBlock) * 4);      // (a scale row is 4 bytes: 512 at most)
+
+    intx8 fx[R][KB];
+    int scale_x[R];
+    auto request = [&](int64_t r0) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int64_t row = min(r0 + 16 * r + l, a.n_rows - 1);
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) fx[r][kb] = load(a.x + row * ld, kb);
+            scale_x[r] = reinterpret_cast<const int*>(a.x_scales)[row];
+        }
+    };
+    const int64_t step = int64_t(gridDim.x) * WR * 16 * R;
+    int64_t r0 = (int64_t(blockIdx.x) * WR + wave / WN) * 16 * R;
+    if (r0 < a.n_rows) request(r0);
+    for (; r0 < a.n_rows; r0 += step) {
+        floatx4 acc[R][NI];
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < NI; ++i) acc[r][i] = floatx4(0.f);
+        auto multiply = [&](auto block) {
+            constexpr int kb = decltype(block)::value;
+            if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int i = 0; i < NI; ++i)
+                        acc[r][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[i][kb], fx[r][kb], acc[r][i], 0, 0, kb, scale_w, kb, scale_x[r]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < NI; ++i) {
+                    const Bf16Fragment w(fw[i][kb], (scale_w >> (8 * kb)) & 255);
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        const Bf16Fragment x(fx[r][kb], (scale_x[r] >> (8 * kb)) & 255);
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) acc[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.f[q], x.f[q], acc[r][i], 0, 0, 0);
+                    }
+                }
             }
+        };
+        multiply(std::integral_constant<int, 0>{});
+        if constexpr (KB > 1) multiply(std::integral_constant<int, 1>{});
+        if constexpr (KB > 2) multiply(std::integral_constant<int, 2>{});
+        if constexpr (KB > 3) multiply(std::integral_constant<int, 3>{});
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < NI; ++i) asm volatile("" : "+v"(acc[r][i]));
+        const int64_t here = r0;
+        if (r0 + step < a.n_rows) request(r0 + step);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int64_t row = here + 16 * r + l;
+            if (row >= a.n_rows) continue;
+            float v[4 * NI];
+#pragma unroll
+            for (int i = 0; i < NI; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) v[4 * i + q] = acc[r][i][q];
+            store_outputs(static_cast<T*>(a.c) + row * a.ldc, n0 + 4 * NI * g, a, v);
+        }
     }
 }
 
 }  // namespace
 
 hipError_t varco_launch_scaled_transform(int dtype, const ScaledArgs& a, hipStream_t stream) {
-    const dim3 grid(unsigned((a.n_rows + kTile - 1) / kTile), unsigned((a.n_out + kTile - 1) / kTile));
+    auto with_type = [&](auto type) {
+        using T = decltype(type);
+        const int32_t blocks = (a.n_in + kCodeBlock - 1) / kCodeBlock;
+        if (blocks > 4) {
+            auto tile = [&](auto wm, auto wn, auto mi) {
+                constexpr int WM = decltype(wm)::value, WN = decltype(wn)::value, MI = decltype(mi)::value;
+                const int64_t tiles_n = (a.n_out + 64 * WN - 1) / (64 * WN), tiles = (a.n_rows + 16 * MI * WM - 1) / (16 * MI * WM) * tiles_n;
+                hipLaunchKernelGGL((scaled_tile_kernel<T, WM, WN, MI>), dim3(unsigned((tiles + 7) / 8 * 8)), dim3(64 * WM * WN), 0, stream, a, int32_t(tiles_n),
+                                   int32_t(tiles));
+            };
+            using std::integral_constant;
+            constexpr int kBig = sizeof(T) == 2 ? 8 : 4;
+            const int64_t big = (a.n_rows + 32 * kBig - 1) / (32 * kBig) * ((a.n_out + 255) / 256);
+            if (a.n_out <= 64)
+                tile(integral_constant<int, 4>{}, integral_constant<int, 1>{}, integral_constant<int, 2>{});
+            else if (big >= 256)
+                tile(integral_constant<int, 2>{}, integral_constant<int, 4>{}, integral_constant<int, kBig>{});
+            else
+                tile(integral_constant<int, 2>{}, integral_constant<int, 2>{}, integral_constant<int, 4>{});
+            return;
+        }
+        auto launch = [&](auto kb, auto wn) {
+            constexpr int KB = decltype(kb)::value, WN = decltype(wn)::value, R = KB == 1 || (KB == 2 && sizeof(T) == 2) ? 2 : 1;
+            constexpr int NI = sizeof(T) == 4 && KB > 2 ? 2 : 4;
+            const int64_t at_once = 16 * R * (4 / WN), columns = (a.n_out + 16 * NI * WN - 1) / (16 * NI * WN);
+            const int64_t groups = std::max<int64_t>(1, std::min<int64_t>((a.n_rows + at_once - 1) / at_once, 1024 / columns));
+            hipLaunchKernelGGL((scaled_rows_kernel<T, KB, NI, WN, R>), dim3(unsigned(groups), unsigned(columns)), dim3(kThreads), 0, stream, a);
+        };
+        auto with_outputs = [&](auto kb) {
+            if (a.n_out <= 64)
+                launch(kb, std::integral_constant<int, 1>{});
+            else if (a.n_out <= 128)
+                launch(kb, std::integral_constant<int, 2>{});
+            else
+                launch(kb, std::integral_constant<int, 4>{});
+        };
+        if (blocks == 1)
+            with_outputs(std::integral_constant<int, 1>{});
+        else if (blocks == 2)
+            with_outputs(std::integral_constant<int, 2>{});
+        else if (blocks == 3)
+            with_outputs(std::integral_constant<int, 3>{});
+        else
+            with_outputs(std::integral_constant<int, 4>{});
+    };
     if (dtype == VARCO_BF16)
-        hipLaunchKernelGGL(scaled_kernel<bf16_t>, grid, dim3(kThreads), 0, stream, a);
+        with_type(bf16_t{});
     else
-        hipLaunchKernelGGL(scaled_kernel<float>, grid, dim3(kThreads), 0, stream, a);
+        with_type(float{});
     return hipGetLastError();
 }
