@@ -50,25 +50,34 @@ struct Bf16Fragment {
     }
 };
 
-// N consecutive outputs of a row, from column n on.
-template <typename T, int N>
-__device__ __forceinline__ void store_outputs(T* row, int32_t n, const ScaledArgs& a, const float (&v)[N]) {
-    constexpr int P = RowPiece<T>::P;
+// Which output (of the 16 NI of a wavefront) row `at` of weight fragment f is. Accumulator v of a lane is row 4 (lane / 16) + v of its
+// fragment; with this order the accumulators of one fragment (fp32) or of two (bf16) are the 16 consecutive bytes of a store, and the four
+// lanes of a row fill 64 bytes with it. (64 consecutive bytes per lane, stored in quarters, fill 64 bytes of a row in four instructions: fp32, 169,343 x
+// 1000 x 1000 546 us against 458.)
+template <typename T>
+__device__ __forceinline__ constexpr int output_of(int f, int at) {
+    return sizeof(T) == 2 ? 32 * (f >> 1) + 8 * (at >> 2) + 4 * (f & 1) + (at & 3) : 16 * f + at;
+}
+
+// A lane's outputs of a row: acc[f] the accumulators of fragment f, n0 the wavefront's first output.
+template <typename T, int NI>
+__device__ __forceinline__ void store_outputs(T* row, int32_t n0, int g, const ScaledArgs& a, const floatx4 (&acc)[NI]) {
+    constexpr int P = RowPiece<T>::P, F = P / 4;
 #pragma unroll
-    for (int i = 0; i < N; i += P) {
+    for (int i = 0; i < NI / F; ++i) {
+        const int32_t n = n0 + output_of<T>(F * i, 4 * g);
         float x[P];
-        if (a.accumulate) {
-            RowPiece<T>::load(row, n + i, a.n_out, x);
+        if (a.accumulate)
+            RowPiece<T>::load(row, n, a.n_out, x);
+        else
 #pragma unroll
-            for (int j = 0; j < P; ++j) x[j] += v[i + j];
-        } else {
+            for (int j = 0; j < P; ++j) x[j] = 0.f;
 #pragma unroll
-            for (int j = 0; j < P; ++j) x[j] = v[i + j];
+        for (int j = 0; j < P; ++j) {
+            x[j] += acc[F * i + j / 4][j % 4];
+            if (a.relu) x[j] = x[j] < 0.f ? 0.f : x[j];         // (NaN stays)
         }
-        if (a.relu)
-#pragma unroll
-            for (int j = 0; j < P; ++j) x[j] = x[j] < 0.f ? 0.f : x[j];         // (NaN stays)
-        RowPiece<T>::store(row, n + i, a.n_out, x);
+        RowPiece<T>::store(row, n, a.n_out, x);
     }
 }
 
@@ -86,9 +95,10 @@ __device__ __forceinline__ void copies_done() {
 }
 
 // Order of a row's 16-byte pieces in LDS: the 16 rows that a fragment takes meet all eight places of a row's 128 bytes. Rows of X are
-// consecutive, those of W are the ones described at scaled_rows_kernel.
+// consecutive, those of W as output_of has them.
 __device__ __forceinline__ int place_x(int row) { return row & 7; }
-__device__ __forceinline__ int place_w(int row) { return (row & 3) | ((row >> 2) & 4); }
+template <typename T>
+__device__ __forceinline__ int place_w(int row) { return sizeof(T) == 2 ? (row & 3) | ((row >> 1) & 4) : row & 7; }
 
 // Long reductions: tiles of 16 MI WM rows x 64 WN outputs, a block of 128 of the reduction at a time through LDS, copied there while the
 // block before is multiplied (two buffers).
@@ -119,7 +129,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void scaled_tile_kernel(ScaledArgs
 #pragma unroll
     for (int h = 0; h < NW; ++h) {
         const int r = (wave * NW + h) * 8 + sub;
-        at_w[h] = uint32_t(min(r, last_n)) * uint32_t(ld) + 16 * ((lane & 7) ^ place_w(r));
+        at_w[h] = uint32_t(min(r, last_n)) * uint32_t(ld) + 16 * ((lane & 7) ^ place_w<T>(r));
     }
     auto copy = [&](int32_t s, uint8_t* lx, uint8_t* lw) {
         const uint8_t* const x = base_x + int64_t(s) * BK;
@@ -134,7 +144,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void scaled_tile_kernel(ScaledArgs
             for (int h = 0; h < NX; ++h) copy_to_lds(piece_x < tail ? x + at_x[h] : zero_piece, lx + (wave * NX + h) * 1024);
 #pragma unroll
             for (int h = 0; h < NW; ++h)
-                copy_to_lds(16 * ((lane & 7) ^ place_w((wave * NW + h) * 8 + sub)) < tail ? w + at_w[h] : zero_piece, lw + (wave * NW + h) * 1024);
+                copy_to_lds(16 * ((lane & 7) ^ place_w<T>((wave * NW + h) * 8 + sub)) < tail ? w + at_w[h] : zero_piece, lw + (wave * NW + h) * 1024);
         }
     };
     // the scales of four blocks at a time
@@ -154,12 +164,11 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void scaled_tile_kernel(ScaledArgs
     auto fragment = [&](const uint8_t* t, int r, int place) {
         return joined(*reinterpret_cast<const uint4*>(t + r * BK + ((g ^ place) << 4)), *reinterpret_cast<const uint4*>(t + r * BK + (((g + 4) ^ place) << 4)));
     };
-    const int row_w = wn + (l >> 2) * 16 + (l & 3);
     auto multiply = [&](const uint8_t* lx, const uint8_t* lw) {
         if constexpr (sizeof(T) == 2) {
             intx8 fw[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) fw[i] = fragment(lw, row_w + 4 * i, place_w(row_w + 4 * i));
+            for (int i = 0; i < 4; ++i) fw[i] = fragment(lw, wn + output_of<T>(i, l), place_w<T>(output_of<T>(i, l)));
             intx8 fx = fragment(lx, wm + l, place_x(l));
 #pragma unroll
             for (int j = 0; j < MI; ++j) {
@@ -173,7 +182,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void scaled_tile_kernel(ScaledArgs
         } else {
             Bf16Fragment fw[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) fw[i] = Bf16Fragment(fragment(lw, row_w + 4 * i, place_w(row_w + 4 * i)), sw & 255);
+            for (int i = 0; i < 4; ++i) fw[i] = Bf16Fragment(fragment(lw, wn + output_of<T>(i, l), place_w<T>(output_of<T>(i, l))), sw & 255);
             intx8 fx = fragment(lx, wm + l, place_x(l));
 #pragma unroll
             for (int j = 0; j < MI; ++j) {
@@ -215,82 +224,114 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void scaled_tile_kernel(ScaledArgs
 #pragma unroll
         for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(acc[j][i]));
         const int64_t row = m0 + wm + 16 * j + l;
-        if (row >= a.n_rows) continue;
-        float v[16];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) v[4 * i + q] = acc[j][i][q];
-        store_outputs(static_cast<T*>(a.c) + row * a.ldc, n0 + wn + 16 * g, a, v);
+        if (row < a.n_rows) store_outputs(static_cast<T*>(a.c) + row * a.ldc, n0 + wn, g, a, acc[j]);
     }
 }
 
 // Short reductions (512 at most): bound by reading X and writing c. A wavefront keeps the weights of 16 NI outputs in registers
-// and walks over rows, 16 R at a time, the next ones requested before the present ones are multiplied; nothing passes through LDS.
-// WN wavefronts of a workgroup take the same rows (their other outputs), which the second to fourth find in the caches.
-// Weight row 4 NI (a / 4) + 4 i + a % 4 of them is row a of fragment i: accumulators 0 .. 3 of the NI fragments are then consecutive
-// outputs of a lane's row, up to 64 bytes to store.
-// NI: 4; 2 where fp32 results take more than 256 columns, whose weights are kept as bf16 (twice the registers).
+// and the workgroup walks over rows, 16 R WR at a time, which are copied to LDS D - 1 steps ahead. WN wavefronts take the same rows, their
+// other outputs. (NI: 4; 2 where fp32 results take more than 256 columns, whose weights are kept as bf16, twice the registers.)
+// Loads and stores are counted together and end in order: a wavefront waits until no more of them are under way than were
+// started after the copies it needs, (D - 2) steps' copies and (D - 1) steps' stores; less may be under way than that only
+// in the first steps and in wavefronts that store by elements, or nothing, which wait until their stores are through as well. Every step starts
+// copies, of the last rows again where there are no more, so that the count holds to the end.
 // (The empty assembly keeps the products in front of the stores' branches: under a branch the lanes that do not take it would
 // supply nothing to the matrix instruction.)
+// 2,449,029 x 512 -> 512 bf16: 839 us, 4.5 TB/s (rows requested into registers one step ahead 1,588; 128 x 128 tiles 1,446); 169,343 x 256 -> 256
+// bf16 35 us (51; 41), fp32 61 us (82; 64).
+template <int N>
+__device__ __forceinline__ void copies_done_but() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
 template <typename T, int KB, int NI, int WN, int R>
-__global__ __launch_bounds__(kThreads, 2) void scaled_rows_kernel(ScaledArgs a) {
-    constexpr int WR = kThreads / 64 / WN;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, l = lane & 15;
+struct RowsLayout {
+    static constexpr int WR = kThreads / 64 / WN, ROWS = 16 * R * WR, COPIES = KB * ROWS * BK / 1024 / 4 + 1, STORES = R * NI * 4 / RowPiece<T>::P;
+    static constexpr int BYTES = KB * ROWS * BK + 4 * 256;
+    static constexpr int D = BYTES > 24 * 1024 ? 3 : 4;
+    static constexpr int BUSY = (D - 2) * COPIES + (D - 1) * STORES;
+    static_assert(BUSY < 64 && ROWS <= 64 && KB * ROWS % 32 == 0, "");
+};
+template <typename T, int KB, int NI, int WN, int R>
+__global__ __launch_bounds__(kThreads, (RowsLayout<T, KB, NI, WN, R>::D * RowsLayout<T, KB, NI, WN, R>::BYTES > 80 * 1024 ? 1 : 2)) void scaled_rows_kernel(ScaledArgs a) {
+    using L = RowsLayout<T, KB, NI, WN, R>;
+    constexpr int WR = L::WR, ROWS = L::ROWS, D = L::D, PER_WAVE = L::COPIES - 1;
+    __shared__ __attribute__((aligned(16))) uint8_t b0[L::BYTES], b1[L::BYTES], b2[L::BYTES], b3[D > 3 ? L::BYTES : 16];       // (apart: see scaled_tile_kernel)
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, l = lane & 15;
     const int32_t n0 = (int32_t(blockIdx.y) * WN + wave % WN) * (16 * NI);
-    if (n0 >= a.n_out) return;                         // (no barriers here)
+    const int wr = wave / WN * (16 * R);
     const uint32_t ld = uint32_t(code_ld(a.n_in));
-    auto load = [&](const uint8_t* row, int kb) {
-        const uint32_t k = kb * kCodeBlock + g * 16;
-        uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo;
-        if (k < ld) lo = *reinterpret_cast<const uint4*>(row + k);
-        if (k + 64 < ld) hi = *reinterpret_cast<const uint4*>(row + k + 64);
-        return joined(lo, hi);
+    const int64_t step = int64_t(gridDim.x) * ROWS, first = int64_t(blockIdx.x) * ROWS;
+
+    // a kilobyte of copies is eight rows of one block of 128 columns: rows 8 (q % (ROWS / 8)) + lane / 8 of block q / (ROWS / 8)
+    const int sub = lane >> 3, piece = 16 * ((lane & 7) ^ sub);
+    auto copy = [&](int64_t r0, uint8_t* to) {
+        const int64_t base = min(r0, a.n_rows - 1);
+        const int last = int(min(int64_t(ROWS), a.n_rows - base)) - 1;
+        const uint8_t* const x = a.x + base * ld;
+#pragma unroll
+        for (int h = 0; h < PER_WAVE; ++h) {
+            const int q = wave * PER_WAVE + h, kb = q / (ROWS / 8), row = q % (ROWS / 8) * 8 + sub;
+            const uint32_t k = kb * kCodeBlock + piece;
+            copy_to_lds(k < ld ? x + (uint32_t(min(row, last)) * ld + k) : zero_piece, to + q * 1024);
+        }
+        const uint8_t* const sc = a.x_scales + (base + min(lane, last)) * 4;         // (a scale row is 4 bytes: 512 columns at most)
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)sc,
+                                         (__attribute__((address_space(3))) void*)(to + KB * ROWS * BK + wave * 256), 4, 0, 0);
     };
+    copy(first, b0);
+    copy(first + step, b1);
+    if constexpr (D > 3) copy(first + 2 * step, b2);
+
     intx8 fw[NI][KB];
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-        const uint8_t* const row = a.w + int64_t(min(n0 + (l >> 2) * (4 * NI) + 4 * i + (l & 3), a.n_out - 1)) * ld;
+        const uint8_t* const row = a.w + int64_t(min(n0 + output_of<T>(i, l), a.n_out - 1)) * ld;
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) fw[i][kb] = load(row, kb);
-    }
-    const int scale_w = *reinterpret_cast<const int*>(a.w_scales + int64_t(n0 / kCodeBlock) * 4);      // (a scale row is 4 bytes: 512 at most)
-
-    intx8 fx[R][KB];
-    int scale_x[R];
-    auto request = [&](int64_t r0) {
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int64_t row = min(r0 + 16 * r + l, a.n_rows - 1);
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb) fx[r][kb] = load(a.x + row * ld, kb);
-            scale_x[r] = reinterpret_cast<const int*>(a.x_scales)[row];
+        for (int kb = 0; kb < KB; ++kb) {
+            const uint32_t k = kb * kCodeBlock + g * 16;
+            uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo;
+            if (k < ld) lo = *reinterpret_cast<const uint4*>(row + k);
+            if (k + 64 < ld) hi = *reinterpret_cast<const uint4*>(row + k + 64);
+            fw[i][kb] = joined(lo, hi);
         }
-    };
-    const int64_t step = int64_t(gridDim.x) * WR * 16 * R;
-    int64_t r0 = (int64_t(blockIdx.x) * WR + wave / WN) * 16 * R;
-    if (r0 < a.n_rows) request(r0);
-    for (; r0 < a.n_rows; r0 += step) {
+    }
+    const int scale_w = *reinterpret_cast<const int*>(a.w_scales + int64_t(min(n0, a.n_out - 1) / kCodeBlock) * 4);
+    const bool regular = n0 + 16 * NI <= a.n_out;
+    int filled = 0;                                     // steps that have stored
+
+    auto walk = [&](int64_t r0, const uint8_t* now, uint8_t* next) {
+        if (regular && filled >= D - 1)
+            copies_done_but<L::BUSY>();
+        else
+            copies_done_but<(D - 2) * L::COPIES>();
+        ++filled;
+        copy(r0 + (D - 1) * step, next);
         floatx4 acc[R][NI];
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int i = 0; i < NI; ++i) acc[r][i] = floatx4(0.f);
+        int scale_x[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) scale_x[r] = *reinterpret_cast<const int*>(now + KB * ROWS * BK + wave * 256 + (wr + 16 * r + l) * 4);
         auto multiply = [&](auto block) {
             constexpr int kb = decltype(block)::value;
-            if constexpr (sizeof(T) == 2) {
+            auto fragment = [&](int r) {
+                const uint8_t* const row = now + kb * ROWS * BK + (wr + 16 * r + l) * BK;
+                return joined(*reinterpret_cast<const uint4*>(row + ((g ^ place_x(l)) << 4)), *reinterpret_cast<const uint4*>(row + (((g + 4) ^ place_x(l)) << 4)));
+            };
 #pragma unroll
-                for (int r = 0; r < R; ++r)
+            for (int r = 0; r < R; ++r) {
+                if constexpr (sizeof(T) == 2) {
+                    const intx8 fx = fragment(r);
 #pragma unroll
                     for (int i = 0; i < NI; ++i)
-                        acc[r][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[i][kb], fx[r][kb], acc[r][i], 0, 0, kb, scale_w, kb, scale_x[r]);
-            } else {
+                        acc[r][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[i][kb], fx, acc[r][i], 0, 0, kb, scale_w, kb, scale_x[r]);
+                } else {
+                    const Bf16Fragment x(fragment(r), (scale_x[r] >> (8 * kb)) & 255);
 #pragma unroll
-                for (int i = 0; i < NI; ++i) {
-                    const Bf16Fragment w(fw[i][kb], (scale_w >> (8 * kb)) & 255);
-#pragma unroll
-                    for (int r = 0; r < R; ++r) {
-                        const Bf16Fragment x(fx[r][kb], (scale_x[r] >> (8 * kb)) & 255);
+                    for (int i = 0; i < NI; ++i) {
+                        const Bf16Fragment w(fw[i][kb], (scale_w >> (8 * kb)) & 255);
 #pragma unroll
                         for (int q = 0; q < 4; ++q) acc[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.f[q], x.f[q], acc[r][i], 0, 0, 0);
                     }
@@ -302,22 +343,24 @@ __global__ __launch_bounds__(kThreads, 2) void scaled_rows_kernel(ScaledArgs a) 
         if constexpr (KB > 2) multiply(std::integral_constant<int, 2>{});
         if constexpr (KB > 3) multiply(std::integral_constant<int, 3>{});
 #pragma unroll
-        for (int r = 0; r < R; ++r)
+        for (int r = 0; r < R; ++r) {
 #pragma unroll
             for (int i = 0; i < NI; ++i) asm volatile("" : "+v"(acc[r][i]));
-        const int64_t here = r0;
-        if (r0 + step < a.n_rows) request(r0 + step);
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int64_t row = here + 16 * r + l;
-            if (row >= a.n_rows) continue;
-            float v[4 * NI];
-#pragma unroll
-            for (int i = 0; i < NI; ++i)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) v[4 * i + q] = acc[r][i][q];
-            store_outputs(static_cast<T*>(a.c) + row * a.ldc, n0 + 4 * NI * g, a, v);
+            const int64_t row = r0 + wr + 16 * r + l;
+            if (row < a.n_rows) store_outputs(static_cast<T*>(a.c) + row * a.ldc, n0, g, a, acc[r]);
         }
+    };
+    for (int64_t r0 = first; r0 < a.n_rows;) {
+        walk(r0, b0, D > 3 ? b3 : b2);
+        if ((r0 += step) >= a.n_rows) break;
+        walk(r0, b1, b0);
+        if ((r0 += step) >= a.n_rows) break;
+        walk(r0, b2, b1);
+        if constexpr (D > 3) {
+            if ((r0 += step) >= a.n_rows) break;
+            walk(r0, b3, b2);
+        }
+        r0 += step;
     }
 }
 
@@ -346,10 +389,13 @@ hipError_t varco_launch_scaled_transform(int dtype, const ScaledArgs& a, hipStre
             return;
         }
         auto launch = [&](auto kb, auto wn) {
-            constexpr int KB = decltype(kb)::value, WN = decltype(wn)::value, R = KB == 1 || (KB == 2 && sizeof(T) == 2) ? 2 : 1;
+            constexpr int KB = decltype(kb)::value, WN = decltype(wn)::value, R = WN == 4 ? 2 : 1;
             constexpr int NI = sizeof(T) == 4 && KB > 2 ? 2 : 4;
-            const int64_t at_once = 16 * R * (4 / WN), columns = (a.n_out + 16 * NI * WN - 1) / (16 * NI * WN);
-            const int64_t groups = std::max<int64_t>(1, std::min<int64_t>((a.n_rows + at_once - 1) / at_once, 1024 / columns));
+            using L = RowsLayout<T, KB, NI, WN, R>;
+            const int64_t columns = (a.n_out + 16 * NI * WN - 1) / (16 * NI * WN), steps = (a.n_rows + L::ROWS - 1) / L::ROWS;
+            // workgroups that are resident together, all columns of the same rows on one XCD (a multiple of 8 in a row of the grid)
+            constexpr int kResident = std::max(1, std::min(KB <= 2 && sizeof(T) == 2 ? 3 : 2, 160 * 1024 / (L::D * L::BYTES)));
+            const int64_t groups = std::min(steps, std::max<int64_t>(8, 256 * kResident / columns / 8 * 8));
             hipLaunchKernelGGL((scaled_rows_kernel<T, KB, NI, WN, R>), dim3(unsigned(groups), unsigned(columns)), dim3(kThreads), 0, stream, a);
         };
         auto with_outputs = [&](auto kb) {
