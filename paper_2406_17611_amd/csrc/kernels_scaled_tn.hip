@@ -5,6 +5,8 @@
 // are transposed when they are read (ds_read_b64_tr_b16 hands lane i of a group of 16 the i-th column of a 4 x 16 block). Row pitch: 64
 // bytes more than a multiple of 256, so that the four rows of such a block start in four different quarters of the banks.
 // The rows are cut into slabs, one workgroup per slab and tile; the slabs' sums are added by a second launch in one order.
+// 2,449,029 rows, 512 x 512: 1,240 us, 1,030 TFLOP/s; bound by the LDS that feeds the matrix units. (Codes requested when they are needed, one
+// buffer, tiles of 128 x 128: 3,260 us.) 169,343 rows, 256 x 256: 51 us, a third of it the partial sums.
 #include <algorithm>
 
 #include "codes_device.h"
@@ -18,10 +20,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef short shortx8 __attribute__((ext_vector_type(8)));
 
-constexpr int kThreads = 256;
-constexpr int kTile = 128;           // inputs and outputs of a tile; a wavefront takes 64 x 64
-constexpr int BK = 32;               // rows of a stage
-constexpr int kPitch = kTile * 2 + 64;
+constexpr int kThreads = 256;        // of the sum over slabs
 
 // Sixteen codes as bf16.
 __device__ __forceinline__ void to_bf16(const uint4& q, float scale, uint4 (&out)[2]) {
@@ -36,70 +35,120 @@ __device__ __forceinline__ void to_bf16(const uint4& q, float scale, uint4 (&out
 }
 
 // Fragment of 16 columns x 32 rows whose first column's element of row 0 (this lane's share of the block) is at LDS byte `at`.
+template <int PITCH>
 __device__ __forceinline__ bf16x8 fragment(uint32_t at) {
     using P = __attribute__((address_space(3))) shortx4*;
     const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)at);
-    const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(at + 4 * kPitch));
+    const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(at + 4 * PITCH));
     return __builtin_bit_cast(bf16x8, shortx8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
 }
 
-__global__ __launch_bounds__(kThreads) void scaled_tn_kernel(ScaledWeightArgs a, int32_t split, int64_t rows_per_split) {
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * BK * kPitch];
-    const int32_t i0 = int32_t(blockIdx.y) * kTile, j0 = int32_t(blockIdx.z) * kTile;
-    const int64_t r0 = int64_t(blockIdx.x) * rows_per_split, r1 = min(a.n_rows, r0 + rows_per_split);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int wi = (wave >> 1) * 64, wj = (wave & 1) * 64;
-    floatx4 acc[4][4];
+// One operand's share of a stage: BK rows of W columns in pieces of 16 codes, dealt to the threads row by row.
+template <int W, int BK, int THREADS>
+struct Slab {
+    static constexpr int PER_ROW = W / 16, N = PER_ROW * BK / THREADS, ROWS = THREADS / PER_ROW, PITCH = W * 2 + 64;
+    static_assert(N * THREADS == PER_ROW * BK && ROWS * PER_ROW == THREADS, "every thread takes as many pieces, of the same columns");
+    const uint8_t* codes;
+    const uint8_t* scales;
+    int64_t ld, lds;
+    bool inside;
+    uint4 q[N];
+    uint32_t s[N];
+    __device__ __forceinline__ void start(const uint8_t* c, const uint8_t* sc, int32_t width, int32_t c0) {
+        const int32_t col = c0 + 16 * int32_t(threadIdx.x % PER_ROW);
+        ld = code_ld(width), lds = scale_ld(width);
+        inside = col < ld;                             // (a piece is whole or not there)
+        codes = c + min(int64_t(col), ld - 16), scales = sc + min(col, width - 1) / kCodeBlock;
+    }
+    // rows r .. r + BK - 1; those from `end` on are repeated ones until they are stored
+    __device__ __forceinline__ void load(int64_t r, int64_t end) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = floatx4(0.f);
-    const uint32_t base = uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)lds));
-    const uint32_t row = 8 * (lane >> 4) + ((lane >> 2) & 3), sub = 8 * (lane & 3);
-    const uint32_t at_y = base + row * kPitch + sub + wi * 2, at_d = base + BK * kPitch + row * kPitch + sub + wj * 2;
-
-    // a stage of 32 rows has 8 pieces of 16 codes per row and operand: one per thread
-    const int tr = threadIdx.x >> 3, tp = threadIdx.x & 7;
-    auto load = [&](const uint8_t* codes, const uint8_t* scales, int32_t width, int32_t c0, int64_t r, uint4& q, float& scale) {
-        const int64_t ld = code_ld(width);
-        const int32_t c = c0 + 16 * tp;
-        q = make_uint4(0u, 0u, 0u, 0u), scale = 1.f;
-        if (r >= r1 || c >= ld) return;
-        q = *reinterpret_cast<const uint4*>(codes + r * ld + c);
-        const uint32_t s = scales[r * scale_ld(width) + c0 / kCodeBlock];
-        scale = __uint_as_float(s ? s << 23 : 0x400000u);
-    };
-    for (int64_t r = r0; r < r1; r += BK) {
-        uint4 qy, qd, out[2];
-        float sy, sd;
-        load(a.y, a.y_scales, a.n_in, i0, r + tr, qy, sy);
-        load(a.d, a.d_scales, a.n_out, j0, r + tr, qd, sd);
-        __syncthreads();
-        to_bf16(qy, sy, out);
-        uint4* p = reinterpret_cast<uint4*>(lds + tr * kPitch + tp * 32);
-        p[0] = out[0], p[1] = out[1];
-        to_bf16(qd, sd, out);
-        p = reinterpret_cast<uint4*>(lds + (BK + tr) * kPitch + tp * 32);
-        p[0] = out[0], p[1] = out[1];
-        __syncthreads();
-        bf16x8 fd[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) fd[j] = fragment(at_d + j * 32);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const bf16x8 fy = fragment(at_y + i * 32);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fy, fd[j], acc[i][j], 0, 0, 0);
+        for (int h = 0; h < N; ++h) {
+            const int64_t row = min(r + int32_t(threadIdx.x / PER_ROW) + h * ROWS, end - 1);
+            q[h] = *reinterpret_cast<const uint4*>(codes + row * ld);
+            s[h] = scales[row * lds];
         }
     }
+    __device__ __forceinline__ void store(uint8_t* to, int64_t r, int64_t end) const {
+#pragma unroll
+        for (int h = 0; h < N; ++h) {
+            const int32_t row = int32_t(threadIdx.x / PER_ROW) + h * ROWS;
+            uint4 out[2];
+            to_bf16(inside && r + row < end ? q[h] : make_uint4(0u, 0u, 0u, 0u), __uint_as_float(s[h] ? s[h] << 23 : 0x400000u), out);
+            uint4* const p = reinterpret_cast<uint4*>(to + row * PITCH + (threadIdx.x % PER_ROW) * 32);
+            p[0] = out[0], p[1] = out[1];
+        }
+    }
+};
+
+template <int WI, int WJ, int MI, int NJ, int BK>
+struct Tile {
+    static constexpr int BI = 16 * MI * WI, BJ = 16 * NJ * WJ, THREADS = 64 * WI * WJ, STAGE = BK;
+    using Y = Slab<BI, BK, THREADS>;
+    using D = Slab<BJ, BK, THREADS>;
+    static constexpr int BYTES = 2 * BK * (Y::PITCH + D::PITCH);
+};
+
+// Work is numbered slab after slab and dealt to the 8 XCDs in runs, so that the tiles of a slab share its rows in the L2 of one (or two). While a stage is multiplied the next one is
+// on its way to registers; it goes to the other of two buffers when the products have been issued.
+template <int WI, int WJ, int MI, int NJ, int BK>
+__global__ __launch_bounds__(64 * WI * WJ, 2) void scaled_tn_kernel(ScaledWeightArgs a, int32_t split, int64_t rows_per_split, int32_t tiles_j, int32_t tiles) {
+    using L = Tile<WI, WJ, MI, NJ, BK>;
+    constexpr int PY = L::Y::PITCH, PD = L::D::PITCH;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[L::BYTES];
+    const int32_t run = (split * tiles + 7) / 8, work = int32_t(blockIdx.x & 7) * run + int32_t(blockIdx.x >> 3);
+    if (work >= split * tiles) return;                  // whole workgroup
+    const int32_t slab = work / tiles, tile = work % tiles;
+    const int32_t i0 = tile / tiles_j * L::BI, j0 = tile % tiles_j * L::BJ;
+    const int64_t r0 = slab * rows_per_split, r1 = min(a.n_rows, r0 + rows_per_split);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wi = wave / WJ * (16 * MI), wj = wave % WJ * (16 * NJ);
+    floatx4 acc[MI][NJ];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] = floatx4(0.f);
+    const uint32_t base = uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)lds));
+    const uint32_t row = 8 * (lane >> 4) + ((lane >> 2) & 3), sub = 8 * (lane & 3);
+    constexpr int kY = BK * PY, kD = BK * PD;
+    const uint32_t at_y = base + row * PY + sub + wi * 2, at_d = base + 2 * kY + row * PD + sub + wj * 2;
+
+    typename L::Y y;
+    typename L::D d;
+    y.start(a.y, a.y_scales, a.n_in, i0);
+    d.start(a.d, a.d_scales, a.n_out, j0);
+    if (r0 < r1) {
+        y.load(r0, r1), d.load(r0, r1);
+        y.store(lds, r0, r1), d.store(lds + 2 * kY, r0, r1);
+    }
+    __syncthreads();
+    uint32_t buf = 0;
+    for (int64_t r = r0; r < r1; r += BK, buf ^= 1u) {
+        const bool more = r + BK < r1;
+        if (more) y.load(r + BK, r1), d.load(r + BK, r1);
+#pragma unroll
+        for (int h = 0; h < BK / 32; ++h) {
+            bf16x8 fd[NJ];
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) fd[j] = fragment<PD>(at_d + buf * kD + h * 32 * PD + j * 32);
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                const bf16x8 fy = fragment<PY>(at_y + buf * kY + h * 32 * PY + i * 32);
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fy, fd[j], acc[i][j], 0, 0, 0);
+            }
+        }
+        if (more) y.store(lds + (buf ^ 1u) * kY, r + BK, r1), d.store(lds + 2 * kY + (buf ^ 1u) * kD, r + BK, r1);
+        __syncthreads();
+    }
     // accumulator v of a lane is element (4 (lane / 16) + v, lane % 16)
-    float* const out = split > 1 ? a.partial + int64_t(blockIdx.x) * a.n_in * a.n_out : a.dh;
+    float* const out = split > 1 ? a.partial + int64_t(slab) * a.n_in * a.n_out : a.dh;
     const int64_t ldo = split > 1 ? a.n_out : a.ldh;
     const bool add = split == 1 && a.accumulate;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < NJ; ++j)
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
                 const int32_t ri = i0 + wi + 16 * i + 4 * (lane >> 4) + v, cj = j0 + wj + 16 * j + (lane & 15);
@@ -110,38 +159,91 @@ __global__ __launch_bounds__(kThreads) void scaled_tn_kernel(ScaledWeightArgs a,
             }
 }
 
-// dh (+)= the slabs' sums, slab 0 first.
+// dh (+)= the slabs' sums: 128 elements per workgroup, eight shares of the slabs, each from its first slab on, then the shares in turn.
+constexpr int kShares = 8;
 __global__ __launch_bounds__(kThreads) void slab_sum_kernel(const float* __restrict__ partial, int32_t split, int32_t n_in, int32_t n_out, float* dh,
                                                             int64_t ldh, int32_t accumulate) {
-    const int64_t n = int64_t(n_in) * n_out;
-    for (int64_t e = int64_t(blockIdx.x) * kThreads + threadIdx.x; e < n; e += int64_t(gridDim.x) * kThreads) {
-        float x = 0.f;
-        for (int32_t s = 0; s < split; ++s) x += partial[s * n + e];
-        const int64_t i = e / n_out;
-        float* const p = dh + i * ldh + (e - i * n_out);
-        *p = accumulate ? *p + x : x;
+    using Row = RowPiece<float>;
+    __shared__ float shares[kShares][128 + 4];
+    const int64_t n = int64_t(n_in) * n_out, e = int64_t(blockIdx.x) * 128;
+    const int lane = threadIdx.x & 31, share = threadIdx.x >> 5;
+    const int32_t here = int32_t(min(int64_t(128), n - e));
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int32_t s = share; s < split; s += kShares) {
+        float v[4];
+        Row::load(partial + s * n + e, 4 * lane, here, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] += v[i];
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) shares[share][4 * lane + i] = x[i];
+    __syncthreads();
+    if (int(threadIdx.x) >= here) return;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kShares; ++i) sum += shares[i][threadIdx.x];
+    const int64_t at = e + threadIdx.x, row = at / n_out;
+    float* const p = dh + row * ldh + (at - row * n_out);
+    *p = accumulate ? *p + sum : sum;
 }
 
-int64_t slab_rows(int64_t n_rows, int64_t split) { return std::max<int64_t>(1, ((n_rows + split - 1) / split + BK - 1) / BK) * BK; }
+template <int WI, int WJ, int MI, int NJ, int BK>
+void launch(Tile<WI, WJ, MI, NJ, BK>, const ScaledWeightArgs& a, int32_t split, int64_t rows, int32_t tiles_j, int32_t tiles, hipStream_t stream) {
+    hipLaunchKernelGGL((scaled_tn_kernel<WI, WJ, MI, NJ, BK>), dim3(unsigned((int64_t(split) * tiles + 7) / 8 * 8)), dim3(64 * WI * WJ), 0, stream, a, split, rows,
+                       tiles_j, tiles);
+}
+
+// Tiles of 256 x 256 where the weights have more than 128 rows and columns and a workgroup per compute unit gets 512 rows or more; else
+// 128 x 128, and 64 on a side of at most 64. (512 x 512 weights, tiles of 256 / of 128: 20,000 rows, 313 each, 36.9 / 30.8 us; 169,343 rows, 2,646 each,
+// 114 / 168; 256 x 256 over 169,343 rows, 661 each, 50.8 / 58.4.)
+using Big = Tile<2, 4, 8, 4, 64>;
+using Middle = Tile<2, 2, 4, 4, 32>;
+using Narrow = Tile<2, 2, 4, 2, 64>;
+using Flat = Tile<2, 2, 2, 4, 64>;
+using Small = Tile<2, 2, 2, 2, 64>;
+
+// Calls f(tile, workgroups that are wanted).
+template <typename F>
+void with_tile(int64_t n_rows, int32_t n_in, int32_t n_out, F f) {
+    const int64_t big = int64_t((n_in + 255) / 256) * ((n_out + 255) / 256);
+    if (n_in > 128 && n_out > 128 && n_rows * big >= int64_t(256) * 512)
+        f(Big{}, 256);
+    else if (n_in > 64 && n_out > 64)
+        f(Middle{}, 512);
+    else if (n_in > 64)
+        f(Narrow{}, 512);
+    else if (n_out > 64)
+        f(Flat{}, 512);
+    else
+        f(Small{}, 512);
+}
+template <typename L>
+int64_t tiles_of(int32_t n_in, int32_t n_out) { return int64_t((n_in + L::BI - 1) / L::BI) * ((n_out + L::BJ - 1) / L::BJ); }
+int64_t slab_rows(int64_t n_rows, int64_t split, int64_t stage) { return std::max<int64_t>(1, ((n_rows + split - 1) / split + stage - 1) / stage) * stage; }
 
 }  // namespace
 
 int32_t varco_scaled_weight_split(int64_t n_rows, int32_t n_in, int32_t n_out) {
-    const int64_t tiles = int64_t((n_in + kTile - 1) / kTile) * ((n_out + kTile - 1) / kTile);
-    const int64_t split = std::max<int64_t>(1, std::min<int64_t>(512 / tiles, n_rows / 256));
-    const int64_t rows = slab_rows(n_rows, split);
-    return int32_t(std::max<int64_t>(1, (n_rows + rows - 1) / rows));
+    int64_t split = 1;
+    with_tile(n_rows, n_in, n_out, [&](auto tile, int64_t wanted) {
+        using L = decltype(tile);
+        split = std::max<int64_t>(1, std::min<int64_t>(wanted / tiles_of<L>(n_in, n_out), n_rows / 256));
+        const int64_t rows = slab_rows(n_rows, split, L::STAGE);
+        split = std::max<int64_t>(1, (n_rows + rows - 1) / rows);
+    });
+    return int32_t(split);
 }
 
 hipError_t varco_launch_scaled_bwd_weight(const ScaledWeightArgs& a, hipStream_t stream) {
     const int32_t split = varco_scaled_weight_split(a.n_rows, a.n_in, a.n_out);
-    const int64_t rows = slab_rows(a.n_rows, split);
-    const dim3 grid{unsigned(split), unsigned((a.n_in + kTile - 1) / kTile), unsigned((a.n_out + kTile - 1) / kTile)};
-    hipLaunchKernelGGL(scaled_tn_kernel, grid, dim3(kThreads), 0, stream, a, split, rows);
+    with_tile(a.n_rows, a.n_in, a.n_out, [&](auto tile, int64_t) {
+        using L = decltype(tile);
+        launch(L{}, a, split, slab_rows(a.n_rows, split, L::STAGE), int32_t((a.n_out + L::BJ - 1) / L::BJ), int32_t(tiles_of<L>(a.n_in, a.n_out)), stream);
+    });
     if (split > 1) {
         const int64_t n = int64_t(a.n_in) * a.n_out;
-        hipLaunchKernelGGL(slab_sum_kernel, dim3(unsigned(std::min<int64_t>((n + kThreads - 1) / kThreads, 2048))), dim3(kThreads), 0, stream, a.partial, split,
+        hipLaunchKernelGGL(slab_sum_kernel, dim3(unsigned((n + 127) / 128)), dim3(kThreads), 0, stream, a.partial, split,
                            a.n_in, a.n_out, a.dh, a.ldh, a.accumulate);
     }
     return hipGetLastError();
