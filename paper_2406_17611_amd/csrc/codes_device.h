@@ -64,47 +64,85 @@ __device__ __forceinline__ float lanes_max(float x) {
     return over_lanes<N>(x, [](float a, float b) { return fmaxf(a, b); });
 }
 
-// A row in pieces of 16 bytes of its storage type, converted to fp32: any address of an element, any length.
+// A row in pieces of 16 bytes of its storage type, converted to fp32, from any address of an element. ANY: of any length; the piece that
+// the last column ends in is loaded from before it, so that it does not leave the row, and moved down; by how much is the same in
+// all lanes. (1,000,000 bf16 rows of 47, norm and codes 91 us; 160 with the last piece by elements.) Else of whole pieces.
 template <typename T>
 struct RowPiece {
     static constexpr int P = 16 / int(sizeof(T));
+    template <bool ANY = true>
     static __device__ __forceinline__ void load(const T* row, int32_t at, int32_t width, float (&v)[P]) {
-        if (at + P <= width) {
-            if constexpr (sizeof(T) == 2) {
-                const uint4 u = load8_any(reinterpret_cast<const char*>(row + at));
-                const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-            } else {
-                typedef float any4 __attribute__((ext_vector_type(4), aligned(4)));
-                const any4 u = *reinterpret_cast<const any4*>(row + at);
-#pragma unroll
-                for (int i = 0; i < P; ++i) v[i] = u[i];
-            }
-        } else {
+        if constexpr (!ANY) {
+            const uint4 u = at < width ? load_16(row + at) : make_uint4(0u, 0u, 0u, 0u);
+            convert(u.x, u.y, u.z, u.w, v);
+            return;
+        }
+        if (width < P) {
 #pragma unroll
             for (int i = 0; i < P; ++i) v[i] = at + i < width ? Elem<T>::load(row + at + i) : 0.f;
+            return;
+        }
+        const uint4 u = load_16(row + min(at, width - P));
+        uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        const int by = width % P ? P - width % P : 0;
+        if (by) {
+            if constexpr (sizeof(T) == 2) {
+                const uint4 m = moved_up8(u, by);
+                const bool ends = at + P > width;
+                w[0] = ends ? m.x : w[0], w[1] = ends ? m.y : w[1], w[2] = ends ? m.z : w[2], w[3] = ends ? m.w : w[3];
+            } else {
+                if (at + P > width) {
+                    w[0] = by == 1 ? w[1] : by == 2 ? w[2] : w[3];
+                    w[1] = by == 1 ? w[2] : by == 2 ? w[3] : 0u;
+                    w[2] = by == 1 ? w[3] : 0u;
+                    w[3] = 0u;
+                }
+            }
+        }
+        const bool none = at >= width;
+        convert(none ? 0u : w[0], none ? 0u : w[1], none ? 0u : w[2], none ? 0u : w[3], v);
+    }
+    static __device__ __forceinline__ void convert(uint32_t x, uint32_t y, uint32_t z, uint32_t t, float (&v)[P]) {
+        const uint32_t w[4] = {x, y, z, t};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(T) == 2)
+                v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+            else
+                v[i] = __uint_as_float(w[i]);
         }
     }
+    static __device__ __forceinline__ uint4 load_16(const T* p) {
+        typedef uint32_t any4 __attribute__((ext_vector_type(4), aligned(2)));
+        const any4 u = *reinterpret_cast<const any4*>(p);
+        return make_uint4(u[0], u[1], u[2], u[3]);
+    }
+    template <bool ANY = true>
     static __device__ __forceinline__ void store(T* row, int32_t at, int32_t width, const float (&v)[P]) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(T) == 2)
+                w[i] = bf16_pair(v[2 * i], v[2 * i + 1]);
+            else
+                w[i] = __float_as_uint(v[i]);
+        }
         if (at + P <= width) {
+            typedef uint32_t any4 __attribute__((ext_vector_type(4), aligned(2)));
+            *reinterpret_cast<any4*>(row + at) = any4{w[0], w[1], w[2], w[3]};
+        } else if (ANY && at < width) {                // what is left, by its binary digits (the same in all lanes)
+            typedef uint32_t any2 __attribute__((ext_vector_type(2), aligned(2)));
+            typedef uint32_t any1 __attribute__((aligned(2)));
+            const int left = width % P;
+            T* const p = row + at;
             if constexpr (sizeof(T) == 2) {
-                typedef uint32_t any4 __attribute__((ext_vector_type(4), aligned(2)));
-                any4 u;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) u[i] = bf16_pair(v[2 * i], v[2 * i + 1]);
-                *reinterpret_cast<any4*>(row + at) = u;
+                if (left & 4) *reinterpret_cast<any2*>(p) = any2{w[0], w[1]};
+                if (left & 2) *reinterpret_cast<any1*>(p + (left & 4)) = left & 4 ? w[2] : w[0];
+                if (left & 1) p[left - 1].bits = uint16_t(left == 1 ? w[0] : left == 3 ? w[1] : left == 5 ? w[2] : w[3]);
             } else {
-                typedef float any4 __attribute__((ext_vector_type(4), aligned(4)));
-                any4 u;
-#pragma unroll
-                for (int i = 0; i < P; ++i) u[i] = v[i];
-                *reinterpret_cast<any4*>(row + at) = u;
+                if (left & 2) *reinterpret_cast<any2*>(p) = any2{w[0], w[1]};
+                if (left & 1) *reinterpret_cast<any1*>(p + left - 1) = left == 1 ? w[0] : w[2];
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < P; ++i)
-                if (at + i < width) Elem<T>::store(row + at + i, v[i]);
         }
     }
     // The value that a stored element holds.

@@ -4,6 +4,7 @@
 // Two launches per 128 tensors: sums of squares per workgroup, then each workgroup of the second launch adds those few
 // sums itself, in one order, instead of a third launch that does it once.
 #include <algorithm>
+#include <type_traits>
 
 #include "codes_device.h"
 #include "varco_scaled.h"
@@ -11,24 +12,24 @@
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTensors = 128;        // of one launch: their table is a kernel argument (4 KiB at most)
-constexpr int kMostPartials = 1024;  // sums of squares over all launches, but for one per launch more
+constexpr int kTensors = 128;        // of one launch: their table is a kernel argument (4 KiB at most; 16 tensors, as a network of a few layers has, fill a smaller one)
+constexpr int kFewTensors = 16;
+constexpr int kWorkgroups = 1024;    // that sum the squares of one launch
 
 // Tensors are cut into chunks, numbered through the tensors of a launch.
+template <int N>
 struct Table {
-    const void* src[kTensors];
-    int64_t n[kTensors];
-    int32_t first[kTensors + 1];
+    static constexpr int kMost = N;
+    const void* src[N];
+    int64_t n[N];
+    int32_t first[N + 1];
     int32_t tensors, chunk;          // elements of a chunk: a multiple of 1024
 };
-struct OutTable {
-    const void* src[kTensors];
-    void* dst[kTensors];
-    int64_t n[kTensors];
-    int32_t first[kTensors + 1];
-    int32_t tensors, chunk;
+template <int N>
+struct OutTable : Table<N> {
+    void* dst[N];
 };
-static_assert(sizeof(OutTable) + 64 <= 4096, "a kernel's arguments");
+static_assert(sizeof(OutTable<kTensors>) + 64 <= 4096, "a kernel's arguments");
 
 // The tensor that chunk c belongs to.
 template <typename TABLE>
@@ -57,8 +58,8 @@ __device__ __forceinline__ double block_sum(double x) {
     return part[0];
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void square_sums_kernel(Table t, double* partial) {
+template <typename T, typename TABLE>
+__global__ __launch_bounds__(kThreads) void square_sums_kernel(TABLE t, double* partial) {
     using Row = RowPiece<T>;
     constexpr int P = Row::P;
     double sum[4] = {0.0, 0.0, 0.0, 0.0};
@@ -68,13 +69,19 @@ __global__ __launch_bounds__(kThreads) void square_sums_kernel(Table t, double* 
         const int64_t at = int64_t(c - t.first[k]) * t.chunk;
         const T* const p = static_cast<const T*>(t.src[k]) + at;
         const int32_t n = int32_t(min(int64_t(t.chunk), t.n[k] - at));
+        auto add = [&](auto any) {
 #pragma unroll 4
-        for (int32_t i = threadIdx.x * P; i < n; i += kThreads * P) {
-            float v[P];
-            Row::load(p, i, n, v);
+            for (int32_t i = threadIdx.x * P; i < n; i += kThreads * P) {
+                float v[P];
+                Row::template load<decltype(any)::value>(p, i, n, v);
 #pragma unroll
-            for (int j = 0; j < P; ++j) sum[j & 3] = fma(double(v[j]), double(v[j]), sum[j & 3]);
-        }
+                for (int j = 0; j < P; ++j) sum[j & 3] = fma(double(v[j]), double(v[j]), sum[j & 3]);
+            }
+        };
+        if (n % P)
+            add(std::true_type{});
+        else
+            add(std::false_type{});
     }
     const double total = block_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
     if (threadIdx.x == 0) partial[blockIdx.x] = total;
@@ -95,8 +102,8 @@ __global__ __launch_bounds__(kThreads) void norm_out_kernel(const double* partia
 }
 
 // STEP: dst -= lr f src (fp32), else dst = f src.
-template <typename T, bool STEP>
-__global__ __launch_bounds__(kThreads) void scale_kernel(OutTable t, const double* partial, int32_t n_partial, float max_norm, float lr, float* out) {
+template <typename T, bool STEP, typename TABLE>
+__global__ __launch_bounds__(kThreads) void scale_kernel(TABLE t, const double* partial, int32_t n_partial, float max_norm, float lr, float* out) {
     using Row = RowPiece<T>;
     constexpr int P = Row::P;
     float f = factor_of(partial, n_partial, max_norm, blockIdx.x == 0 ? out : nullptr);
@@ -110,15 +117,22 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(OutTable t, const doubl
         T* const q = static_cast<T*>(t.dst[k]) + at;
         if (!STEP && same && p == q) continue;             // in place and within the limit: the elements stay as they are
         const int32_t n = int32_t(min(int64_t(t.chunk), t.n[k] - at));
+        auto scale = [&](auto any) {
+            constexpr bool ANY = decltype(any)::value;
 #pragma unroll 4
-        for (int32_t i = threadIdx.x * P; i < n; i += kThreads * P) {
-            float v[P], w[P];
-            Row::load(p, i, n, v);
-            if (STEP) Row::load(q, i, n, w);
+            for (int32_t i = threadIdx.x * P; i < n; i += kThreads * P) {
+                float v[P], w[P];
+                Row::template load<ANY>(p, i, n, v);
+                if (STEP) Row::template load<ANY>(q, i, n, w);
 #pragma unroll
-            for (int j = 0; j < P; ++j) v[j] = STEP ? fmaf(-f, v[j], w[j]) : f * v[j];
-            Row::store(q, i, n, v);
-        }
+                for (int j = 0; j < P; ++j) v[j] = STEP ? fmaf(-f, v[j], w[j]) : f * v[j];
+                Row::template store<ANY>(q, i, n, v);
+            }
+        };
+        if (n % P)
+            scale(std::true_type{});
+        else
+            scale(std::false_type{});
     }
 }
 
@@ -141,13 +155,7 @@ void over_launches(int32_t n_tensors, const int64_t* sizes, int64_t chunk, F f) 
         if (chunks) f(i, n, chunks);
     }
 }
-// Workgroups of a launch of the first kernel: its share of kMostPartials by its share of the elements, rounded up.
-int64_t workgroups(int64_t chunks, int64_t all) { return std::max<int64_t>(1, std::min(chunks, (kMostPartials * chunks + all - 1) / all)); }
-int64_t all_chunks(int32_t n_tensors, const int64_t* sizes, int64_t chunk) {
-    int64_t all = 0;
-    for (int32_t i = 0; i < n_tensors; ++i) all += chunks_of(sizes[i], chunk);
-    return all;
-}
+int64_t workgroups(int64_t chunks) { return std::min<int64_t>(chunks, kWorkgroups); }
 template <typename TABLE>
 void fill(TABLE& t, int32_t i, int32_t n, const void* const* src, const int64_t* sizes, int32_t chunk) {
     int64_t c = 0;
@@ -159,17 +167,28 @@ void fill(TABLE& t, int32_t i, int32_t n, const void* const* src, const int64_t*
     t.tensors = n, t.chunk = chunk;
 }
 
+template <typename F>
+void with_table(int32_t tensors, F f) {
+    if (tensors <= kFewTensors)
+        f(std::integral_constant<int, kFewTensors>{});
+    else
+        f(std::integral_constant<int, kTensors>{});
+}
+
 template <typename T, bool STEP>
 hipError_t launch_scale(int32_t n_tensors, const void* const* src, void* const* dst, const int64_t* sizes, const double* partial, int32_t n_partial,
                         float max_norm, float lr, float* out, hipStream_t stream) {
     const int32_t chunk = chunk_of(total_of(n_tensors, sizes));
     hipError_t err = hipSuccess;
     over_launches(n_tensors, sizes, chunk, [&](int32_t i, int32_t n, int64_t chunks) {
-        OutTable t;
-        fill(t, i, n, src, sizes, chunk);
-        for (int32_t k = 0; k < n; ++k) t.dst[k] = dst[i + k];
-        hipLaunchKernelGGL((scale_kernel<T, STEP>), dim3(unsigned(std::min<int64_t>(chunks, 2048))), dim3(kThreads), 0, stream, t, partial, n_partial,
-                           max_norm, lr, out);
+        with_table(n, [&](auto most) {
+            using TABLE = OutTable<decltype(most)::value>;
+            TABLE t;
+            fill(t, i, n, src, sizes, chunk);
+            for (int32_t k = 0; k < n; ++k) t.dst[k] = dst[i + k];
+            hipLaunchKernelGGL((scale_kernel<T, STEP, TABLE>), dim3(unsigned(std::min<int64_t>(chunks, 2048))), dim3(kThreads), 0, stream, t, partial,
+                               n_partial, max_norm, lr, out);
+        });
         if (err == hipSuccess) err = hipGetLastError();
         out = nullptr;
     });
@@ -180,25 +199,26 @@ hipError_t launch_scale(int32_t n_tensors, const void* const* src, void* const* 
 
 int32_t varco_clip_partials(int32_t n_tensors, const int64_t* sizes) {
     const int32_t chunk = chunk_of(total_of(n_tensors, sizes));
-    const int64_t all = all_chunks(n_tensors, sizes, chunk);
     int64_t n = 0;
-    over_launches(n_tensors, sizes, chunk, [&](int32_t, int32_t, int64_t chunks) { n += workgroups(chunks, all); });
+    over_launches(n_tensors, sizes, chunk, [&](int32_t, int32_t, int64_t chunks) { n += workgroups(chunks); });
     return int32_t(n);
 }
 
 hipError_t varco_launch_square_sums(int dtype, int32_t n_tensors, const void* const* grads, const int64_t* sizes, double* partial,
                                     hipStream_t stream) {
     const int32_t chunk = chunk_of(total_of(n_tensors, sizes));
-    const int64_t all = all_chunks(n_tensors, sizes, chunk);
     hipError_t err = hipSuccess;
     over_launches(n_tensors, sizes, chunk, [&](int32_t i, int32_t n, int64_t chunks) {
-        Table t;
-        fill(t, i, n, grads, sizes, chunk);
-        const int64_t blocks = workgroups(chunks, all);
-        if (dtype == VARCO_BF16)
-            hipLaunchKernelGGL(square_sums_kernel<bf16_t>, dim3(unsigned(blocks)), dim3(kThreads), 0, stream, t, partial);
-        else
-            hipLaunchKernelGGL(square_sums_kernel<float>, dim3(unsigned(blocks)), dim3(kThreads), 0, stream, t, partial);
+        const int64_t blocks = workgroups(chunks);
+        with_table(n, [&](auto most) {
+            using TABLE = Table<decltype(most)::value>;
+            TABLE t;
+            fill(t, i, n, grads, sizes, chunk);
+            if (dtype == VARCO_BF16)
+                hipLaunchKernelGGL((square_sums_kernel<bf16_t, TABLE>), dim3(unsigned(blocks)), dim3(kThreads), 0, stream, t, partial);
+            else
+                hipLaunchKernelGGL((square_sums_kernel<float, TABLE>), dim3(unsigned(blocks)), dim3(kThreads), 0, stream, t, partial);
+        });
         if (err == hipSuccess) err = hipGetLastError();
         partial += blocks;
     });

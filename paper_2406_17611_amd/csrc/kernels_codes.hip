@@ -2,45 +2,35 @@
 // matrix). Elementwise but for the largest size of a block: bound by reading the values once and writing a byte for each.
 #include <algorithm>
 
-#include "codes_device.h"
+#include "row_layout.h"
 #include "varco_scaled.h"
 
 namespace {
 
 constexpr int kThreads = 256;
 
-// A group of 16 (bf16) or 32 (fp32) lanes takes a block of 128 columns, a piece of 16 bytes per lane, so the block's
-// largest element is found without leaving registers. The blocks of a row are numbered through all rows.
-template <typename T, bool GATE>
-__global__ __launch_bounds__(kThreads) void quantize_rows_kernel(int64_t n_rows, int32_t width, const T* x, int64_t ldx, const T* gate, int64_t ldg,
-                                                                 uint8_t* codes, uint8_t* scales) {
+// Rows dealt to lanes as row_layout.h has it: no lane waits for more than the lanes of its scale.
+template <typename T, int G, int E, bool GATE, bool ANY>
+__global__ __launch_bounds__(row_threads(G)) void quantize_rows_kernel(int64_t n_rows, int32_t width, const T* x, int64_t ldx, const T* gate, int64_t ldg,
+                                                                       uint8_t* codes, uint8_t* scales) {
     using Row = RowPiece<T>;
-    constexpr int P = Row::P, G = kCodeBlock / P;
-    const int32_t blocks = (width + kCodeBlock - 1) / kCodeBlock, slots = int32_t(scale_ld(width));
-    const int64_t ldc = code_ld(width), total = n_rows * slots;
+    constexpr int P = Row::P, kRows = row_threads(G) / G;
+    const int64_t ldc = code_ld(width), lds = scale_ld(width);
     const int t = threadIdx.x & (G - 1);
-    for (int64_t i = int64_t(blockIdx.x) * (kThreads / G) + threadIdx.x / G; i < total; i += int64_t(gridDim.x) * (kThreads / G)) {
-        const int64_t row = i / slots;
-        const int32_t b = int32_t(i - row * slots);
-        if (b >= blocks) {                             // the padding of the scales
-            if (t == 0) scales[i] = kOneScale;
-            continue;
-        }
-        const int32_t at = b * kCodeBlock + t * P;
-        float v[P];
-        Row::load(x + row * ldx, at, width, v);
+    for (int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / G; row < n_rows; row += int64_t(gridDim.x) * kRows) {
+        float v[E][P];
+#pragma unroll
+        for (int e = 0; e < E; ++e) Row::template load<ANY>(x + row * ldx, (t + e * G) * P, width, v[e]);
         if constexpr (GATE) {
-            float g[P];
-            Row::load(gate + row * ldg, at, width, g);
+            float g[E][P];
 #pragma unroll
-            for (int j = 0; j < P; ++j) v[j] = g[j] > 0.f ? v[j] : 0.f;
+            for (int e = 0; e < E; ++e) Row::template load<ANY>(gate + row * ldg, (t + e * G) * P, width, g[e]);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+#pragma unroll
+                for (int j = 0; j < P; ++j) v[e][j] = g[e][j] > 0.f ? v[e][j] : 0.f;
         }
-        float a = 0.f;
-#pragma unroll
-        for (int j = 0; j < P; ++j) a = fmaxf(a, finite_size(v[j]));
-        const int e = code_exponent(lanes_max<G>(a));
-        if (at < ldc) Row::store_codes(codes + row * ldc, at, v, code_inverse(e));
-        if (t == 0) scales[i] = uint8_t(e + 127);
+        store_row_codes<T, G, E>(v, t, width, codes + row * ldc, scales + row * lds);
     }
 }
 
@@ -106,21 +96,19 @@ __global__ __launch_bounds__(kThreads) void quantize_weights_kernel(int32_t n_in
 
 hipError_t varco_launch_quantize_rows(int dtype, int64_t n_rows, int32_t width, const void* x, int64_t ldx, const void* gate, int64_t ldg,
                                       uint8_t* codes, uint8_t* scales, hipStream_t stream) {
-    auto go = [&](auto type) {
+    with_type(dtype, [&](auto type) {
         using T = decltype(type);
-        const int64_t groups = n_rows * scale_ld(width), per = kThreads / (kCodeBlock / RowPiece<T>::P);
-        const dim3 grid(unsigned(std::min<int64_t>((groups + per - 1) / per, 256 * 32)));
-        if (gate)
-            hipLaunchKernelGGL((quantize_rows_kernel<T, true>), grid, dim3(kThreads), 0, stream, n_rows, width, static_cast<const T*>(x), ldx,
-                               static_cast<const T*>(gate), ldg, codes, scales);
-        else
-            hipLaunchKernelGGL((quantize_rows_kernel<T, false>), grid, dim3(kThreads), 0, stream, n_rows, width, static_cast<const T*>(x), ldx,
-                               static_cast<const T*>(nullptr), 0, codes, scales);
-    };
-    if (dtype == VARCO_BF16)
-        go(bf16_t{});
-    else
-        go(float{});
+        with_row_layout<T>(width, [&](auto g, auto e) {
+            constexpr int G = decltype(g)::value, E = decltype(e)::value, kRows = row_threads(G) / G;
+            const dim3 grid(unsigned(std::min<int64_t>((n_rows + kRows - 1) / kRows, 256 * 32)));
+            with_bool(gate, [&](auto gated) {
+                with_bool(width % RowPiece<T>::P, [&](auto any) {
+                    hipLaunchKernelGGL((quantize_rows_kernel<T, G, E, decltype(gated)::value, decltype(any)::value>), grid, dim3(row_threads(G)), 0, stream,
+                                       n_rows, width, static_cast<const T*>(x), ldx, static_cast<const T*>(gate), ldg, codes, scales);
+                });
+            });
+        });
+    });
     return hipGetLastError();
 }
 

@@ -5,15 +5,11 @@
 // rows above 2,048 elements are taken by 512 lanes, which meet in LDS.
 // Bound by reading and writing each row once.
 #include <algorithm>
-#include <type_traits>
 
-#include "codes_device.h"
+#include "row_layout.h"
 #include "varco_scaled.h"
 
 namespace {
-
-constexpr int kWide = 512;           // lanes of a wide row: a workgroup
-constexpr int threads_of(int g) { return g > 64 ? g : 256; }
 
 // Sum over the G lanes of a row, in all of them, in one order.
 template <int G>
@@ -32,10 +28,10 @@ __device__ __forceinline__ float row_sum(float x, float* shared) {
     }
 }
 
-template <typename T, int G, int E, bool CODES>
-__global__ __launch_bounds__(threads_of(G)) void rms_norm_kernel(NormFwdArgs a) {
+template <typename T, int G, int E, bool CODES, bool ANY>
+__global__ __launch_bounds__(row_threads(G)) void rms_norm_kernel(NormFwdArgs a) {
     using Row = RowPiece<T>;
-    constexpr int P = Row::P, kRows = threads_of(G) / G, kBlockLanes = kCodeBlock / P;
+    constexpr int P = Row::P, kRows = row_threads(G) / G;
     __shared__ float shared[G > 64 ? G / 64 : 1];
     const int t = threadIdx.x & (G - 1);
     float gain[E][P];
@@ -51,11 +47,11 @@ __global__ __launch_bounds__(threads_of(G)) void rms_norm_kernel(NormFwdArgs a) 
         float v[E][P];
         float sum = 0.f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) Row::load(static_cast<const T*>(a.x) + row * a.ldx, (t + e * G) * P, a.width, v[e]);
+        for (int e = 0; e < E; ++e) Row::template load<ANY>(static_cast<const T*>(a.x) + row * a.ldx, (t + e * G) * P, a.width, v[e]);
         if (a.residual) {
             float r[E][P];
 #pragma unroll
-            for (int e = 0; e < E; ++e) Row::load(static_cast<const T*>(a.residual) + row * a.ldr, (t + e * G) * P, a.width, r[e]);
+            for (int e = 0; e < E; ++e) Row::template load<ANY>(static_cast<const T*>(a.residual) + row * a.ldr, (t + e * G) * P, a.width, r[e]);
 #pragma unroll
             for (int e = 0; e < E; ++e)
 #pragma unroll
@@ -63,7 +59,7 @@ __global__ __launch_bounds__(threads_of(G)) void rms_norm_kernel(NormFwdArgs a) 
         }
         if (a.total)
 #pragma unroll
-            for (int e = 0; e < E; ++e) Row::store(static_cast<T*>(a.total) + row * a.ldt, (t + e * G) * P, a.width, v[e]);
+            for (int e = 0; e < E; ++e) Row::template store<ANY>(static_cast<T*>(a.total) + row * a.ldt, (t + e * G) * P, a.width, v[e]);
 #pragma unroll
         for (int e = 0; e < E; ++e)
 #pragma unroll
@@ -76,36 +72,17 @@ __global__ __launch_bounds__(threads_of(G)) void rms_norm_kernel(NormFwdArgs a) 
             for (int j = 0; j < P; ++j) v[e][j] = v[e][j] * s * gain[e][j];
         if (a.y)
 #pragma unroll
-            for (int e = 0; e < E; ++e) Row::store(static_cast<T*>(a.y) + row * a.ldy, (t + e * G) * P, a.width, v[e]);
-        if constexpr (CODES) {
-            const int64_t ldc = code_ld(a.width), lds = scale_ld(a.width);
-            const int32_t blocks = (a.width + kCodeBlock - 1) / kCodeBlock;
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const int32_t at = (t + e * G) * P;
-                float m = 0.f;
-#pragma unroll
-                for (int j = 0; j < P; ++j) m = fmaxf(m, at + j < a.width ? finite_size(v[e][j]) : 0.f);
-                const int x = code_exponent(lanes_max<(G < kBlockLanes ? G : kBlockLanes)>(m));
-                if (at < ldc) {
-                    float q[P];
-#pragma unroll
-                    for (int j = 0; j < P; ++j) q[j] = at + j < a.width ? v[e][j] : 0.f;
-                    Row::store_codes(a.codes + row * ldc, at, q, code_inverse(x));
-                    if (at % kCodeBlock == 0) a.scales[row * lds + at / kCodeBlock] = uint8_t(x + 127);
-                }
-            }
-            if (t < int(lds) - blocks) a.scales[row * lds + blocks + t] = kOneScale;
-        }
+            for (int e = 0; e < E; ++e) Row::template store<ANY>(static_cast<T*>(a.y) + row * a.ldy, (t + e * G) * P, a.width, v[e]);
+        if constexpr (CODES) store_row_codes<T, G, E>(v, t, a.width, a.codes + row * code_ld(a.width), a.scales + row * scale_ld(a.width));
     }
 }
 
 // dg: every lane sums its own columns over the rows that its group takes; the groups of a workgroup are joined in LDS, the workgroups'
 // sums by a second launch, each in one order. With one workgroup dgain is written at once.
-template <typename T, int G, int E>
-__global__ __launch_bounds__(threads_of(G)) void rms_norm_bwd_kernel(NormBwdArgs a) {
+template <typename T, int G, int E, bool ANY>
+__global__ __launch_bounds__(row_threads(G)) void rms_norm_bwd_kernel(NormBwdArgs a) {
     using Row = RowPiece<T>;
-    constexpr int P = Row::P, kThreads = threads_of(G), kRows = kThreads / G;
+    constexpr int P = Row::P, kThreads = row_threads(G), kRows = kThreads / G;
     __shared__ float shared[G > 64 ? G / 64 : 1];
     __shared__ float joined[kRows > 1 ? kThreads * E * P : 1];
     const int t = threadIdx.x & (G - 1);
@@ -124,8 +101,8 @@ __global__ __launch_bounds__(threads_of(G)) void rms_norm_bwd_kernel(NormBwdArgs
         const float s = a.inv_rms[row];
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            Row::load(static_cast<const T*>(a.dy) + row * a.lddy, (t + e * G) * P, a.width, dy[e]);
-            Row::load(static_cast<const T*>(a.u) + row * a.ldu, (t + e * G) * P, a.width, u[e]);
+            Row::template load<ANY>(static_cast<const T*>(a.dy) + row * a.lddy, (t + e * G) * P, a.width, dy[e]);
+            Row::template load<ANY>(static_cast<const T*>(a.u) + row * a.ldu, (t + e * G) * P, a.width, u[e]);
         }
         float sum = 0.f;
 #pragma unroll
@@ -142,13 +119,13 @@ __global__ __launch_bounds__(threads_of(G)) void rms_norm_bwd_kernel(NormBwdArgs
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             float du[P];
-            if (a.dtotal) Row::load(static_cast<const T*>(a.dtotal) + row * a.lddt, (t + e * G) * P, a.width, du);
+            if (a.dtotal) Row::template load<ANY>(static_cast<const T*>(a.dtotal) + row * a.lddt, (t + e * G) * P, a.width, du);
 #pragma unroll
             for (int j = 0; j < P; ++j) {
                 const float d = s * fmaf(-u[e][j], mean, dy[e][j]);
                 dy[e][j] = a.dtotal ? d + du[j] : d;
             }
-            Row::store(static_cast<T*>(a.dx) + row * a.lddx, (t + e * G) * P, a.width, dy[e]);
+            Row::template store<ANY>(static_cast<T*>(a.dx) + row * a.lddx, (t + e * G) * P, a.width, dy[e]);
         }
     }
     if (!a.dgain) return;
@@ -181,61 +158,23 @@ __global__ __launch_bounds__(threads_of(G)) void rms_norm_bwd_kernel(NormBwdArgs
     }
 }
 
-// dgain (+)= the sum of `n` rows of `partial`: 32 columns per workgroup, 8 shares of the rows, in fp64.
-__global__ __launch_bounds__(256) void gain_sum_kernel(const float* __restrict__ partial, int32_t n, int32_t width, float* dgain, int32_t accumulate) {
-    __shared__ double shares[8][32];
-    const int32_t c = int32_t(blockIdx.x) * 32 + (threadIdx.x & 31);
-    const int part = threadIdx.x >> 5;
+// dgain (+)= the sum of `n` rows of `partial`: 16 columns per workgroup, 64 shares of the rows, in fp64.
+constexpr int kShares = 64;
+__global__ __launch_bounds__(16 * kShares) void gain_sum_kernel(const float* __restrict__ partial, int32_t n, int32_t width, float* dgain, int32_t accumulate) {
+    __shared__ double shares[kShares][16];
+    const int32_t c = int32_t(blockIdx.x) * 16 + (threadIdx.x & 15);
+    const int part = threadIdx.x >> 4;
     double x = 0.0;
     if (c < width)
-        for (int32_t r = part; r < n; r += 8) x += double(partial[int64_t(r) * width + c]);
-    shares[part][threadIdx.x & 31] = x;
+#pragma unroll 4
+        for (int32_t r = part; r < n; r += kShares) x += double(partial[int64_t(r) * width + c]);
+    shares[part][threadIdx.x & 15] = x;
     __syncthreads();
-    if (part == 0 && c < width) {
-        for (int i = 1; i < 8; ++i) x += shares[i][threadIdx.x];
-        dgain[c] = accumulate ? float(double(dgain[c]) + x) : float(x);
+    for (int s = kShares / 2; s > 0; s >>= 1) {
+        if (part < s) shares[part][threadIdx.x & 15] += shares[part + s][threadIdx.x & 15];
+        __syncthreads();
     }
-}
-
-template <int N>
-using Int = std::integral_constant<int, N>;
-
-// Calls f(lanes of a row, pieces per lane) for rows of `width` elements.
-template <typename T, typename F>
-void with_layout(int32_t width, F f) {
-    const int64_t pieces = code_ld(width) / RowPiece<T>::P;
-    if (pieces <= 4)
-        f(Int<4>{}, Int<1>{});
-    else if (pieces <= 8)
-        f(Int<8>{}, Int<1>{});
-    else if (pieces <= 16)
-        f(Int<16>{}, Int<1>{});
-    else if (pieces <= 32)
-        f(Int<32>{}, Int<1>{});
-    else if (pieces <= 64)
-        f(Int<64>{}, Int<1>{});
-    else if (pieces <= 128)
-        f(Int<64>{}, Int<2>{});
-    else if (pieces <= 256)
-        f(Int<64>{}, Int<4>{});
-    else if (pieces <= 512 && sizeof(T) == 4)
-        f(Int<64>{}, Int<8>{});
-    else if (pieces <= kWide)
-        f(Int<kWide>{}, Int<1>{});
-    else if (pieces <= 2 * kWide)
-        f(Int<kWide>{}, Int<2>{});
-    else if (pieces <= 4 * kWide)
-        f(Int<kWide>{}, Int<4>{});
-    else if constexpr (sizeof(T) == 4)
-        f(Int<kWide>{}, Int<8>{});
-}
-
-template <typename F>
-void with_type(int dtype, F f) {
-    if (dtype == VARCO_BF16)
-        f(bf16_t{});
-    else
-        f(float{});
+    if (part == 0 && c < width) dgain[c] = float(accumulate ? double(dgain[c]) + shares[0][threadIdx.x] : shares[0][threadIdx.x]);
 }
 
 }  // namespace
@@ -243,13 +182,14 @@ void with_type(int dtype, F f) {
 hipError_t varco_launch_rms_norm_fwd(int dtype, const NormFwdArgs& a, hipStream_t stream) {
     with_type(dtype, [&](auto type) {
         using T = decltype(type);
-        with_layout<T>(a.width, [&](auto g, auto e) {
-            constexpr int G = decltype(g)::value, E = decltype(e)::value, kRows = threads_of(G) / G;
+        with_row_layout<T>(a.width, [&](auto g, auto e) {
+            constexpr int G = decltype(g)::value, E = decltype(e)::value, kRows = row_threads(G) / G;
             const dim3 grid(unsigned(std::min<int64_t>((a.n_rows + kRows - 1) / kRows, 256 * 16)));
-            if (a.codes)
-                hipLaunchKernelGGL((rms_norm_kernel<T, G, E, true>), grid, dim3(threads_of(G)), 0, stream, a);
-            else
-                hipLaunchKernelGGL((rms_norm_kernel<T, G, E, false>), grid, dim3(threads_of(G)), 0, stream, a);
+            with_bool(a.codes, [&](auto codes) {
+                with_bool(a.width % RowPiece<T>::P, [&](auto any) {
+                    hipLaunchKernelGGL((rms_norm_kernel<T, G, E, decltype(codes)::value, decltype(any)::value>), grid, dim3(row_threads(G)), 0, stream, a);
+                });
+            });
         });
     });
     return hipGetLastError();
@@ -258,8 +198,8 @@ hipError_t varco_launch_rms_norm_fwd(int dtype, const NormFwdArgs& a, hipStream_
 int32_t varco_norm_blocks(int dtype, int64_t n_rows, int32_t width) {
     int64_t blocks = 1;
     with_type(dtype, [&](auto type) {
-        with_layout<decltype(type)>(width, [&](auto g, auto) {
-            constexpr int G = decltype(g)::value, kRows = threads_of(G) / G;
+        with_row_layout<decltype(type)>(width, [&](auto g, auto) {
+            constexpr int G = decltype(g)::value, kRows = row_threads(G) / G;
             blocks = std::max<int64_t>(1, std::min<int64_t>((n_rows + kRows - 1) / kRows, 1024));
         });
     });
@@ -270,13 +210,15 @@ hipError_t varco_launch_rms_norm_bwd(int dtype, const NormBwdArgs& a, hipStream_
     const int32_t blocks = varco_norm_blocks(dtype, a.n_rows, a.width);
     with_type(dtype, [&](auto type) {
         using T = decltype(type);
-        with_layout<T>(a.width, [&](auto g, auto e) {
+        with_row_layout<T>(a.width, [&](auto g, auto e) {
             constexpr int G = decltype(g)::value, E = decltype(e)::value;
-            hipLaunchKernelGGL((rms_norm_bwd_kernel<T, G, E>), dim3(unsigned(blocks)), dim3(threads_of(G)), 0, stream, a);
+            with_bool(a.width % RowPiece<T>::P, [&](auto any) {
+                hipLaunchKernelGGL((rms_norm_bwd_kernel<T, G, E, decltype(any)::value>), dim3(unsigned(blocks)), dim3(row_threads(G)), 0, stream, a);
+            });
         });
     });
     hipError_t err = hipGetLastError();
     if (err != hipSuccess || !a.dgain || blocks == 1) return err;
-    hipLaunchKernelGGL(gain_sum_kernel, dim3(unsigned((a.width + 31) / 32)), dim3(256), 0, stream, a.partial, blocks, a.width, a.dgain, a.accumulate);
+    hipLaunchKernelGGL(gain_sum_kernel, dim3(unsigned((a.width + 15) / 16)), dim3(16 * kShares), 0, stream, a.partial, blocks, a.width, a.dgain, a.accumulate);
     return hipGetLastError();
 }
