@@ -241,13 +241,17 @@ def _refuse(code, text):
     raise VarcoError(code, text)
 
 
+_DTYPES = {}
+
+
 def _dtype(t):
-    name = str(t.dtype)
-    if name == "torch.float32":
-        return F32
-    if name == "torch.bfloat16":
-        return BF16
-    _refuse(ERR_UNSUPPORTED, f"{name}: neither float32 nor bfloat16")
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: F32, torch.bfloat16: BF16})
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        _refuse(ERR_UNSUPPORTED, f"{t.dtype}: neither float32 nor bfloat16")
+    return code
 
 
 def _on_device(*tensors):
@@ -255,7 +259,7 @@ def _on_device(*tensors):
     import torch
     current = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != current):
+        if t is not None and t.get_device() != current:
             _refuse(ERR_INVALID_ARG, f"a tensor on {t.device}, the current device is cuda:{current}")
 
 
@@ -263,13 +267,21 @@ def _matrix(t, shape, like, what):
     """(address, leading dimension) of a matrix whose rows' elements are consecutive; None -> NULL."""
     if t is None:
         return None, 0
-    if t.dim() != 2 or tuple(t.shape) != shape:
-        _refuse(ERR_SHAPE, f"{what}: {tuple(t.shape)} where {shape} is needed")
+    if t.shape != shape:
+        _refuse(ERR_SHAPE, f"{what}: {tuple(t.shape)} where {tuple(shape)} is needed")
     if t.dtype != like:
         _refuse(ERR_UNSUPPORTED, f"{what}: {t.dtype} where {like} is needed")
-    if shape[1] > 1 and t.stride(1) != 1:
+    ld, one = t.stride()
+    if one != 1 and shape[1] > 1:
         _refuse(ERR_SHAPE, f"{what}: the elements of a row are not consecutive")
-    return t.data_ptr(), t.stride(0) if shape[0] > 1 else max(shape[1], 1)
+    return t.data_ptr(), ld if shape[0] > 1 else shape[1]
+
+
+def _rows(t, what):
+    """(rows, width) of a matrix."""
+    if t.dim() != 2:
+        _refuse(ERR_SHAPE, f"{what}: a matrix is needed, got {tuple(t.shape)}")
+    return t.shape
 
 
 def _vector(t, n, what):
@@ -288,7 +300,7 @@ def _code_rows(codes, scales, rows, width, scale_rows, what):
     if codes is None or scales is None:
         _refuse(ERR_INVALID_ARG, f"{what}: codes without scales")
     for t, n, ld in ((codes, rows, code_ld(width)), (scales, scale_rows, scale_ld(width))):
-        if t.element_size() != 1 or tuple(t.shape) != (n, ld) or not t.is_contiguous():
+        if t.element_size() != 1 or t.shape != (n, ld) or not t.is_contiguous():
             _refuse(ERR_SHAPE, f"{what}: {tuple(t.shape)} where {n} whole rows of {ld} bytes are needed")
     return codes.data_ptr(), scales.data_ptr()
 
@@ -310,7 +322,7 @@ def _scratch(need, workspace, device, stream):
 
 def quantize_rows(x, codes, scales, gate=None, stream=None):
     """codes [n, code_ld(width)], scales [n, scale_ld(width)] of the rows of x (of x where gate > 0)."""
-    dt, (n, w) = _dtype(x), tuple(x.shape)
+    dt, (n, w) = _dtype(x), _rows(x, "x")
     _on_device(x, codes, scales, gate)
     px, ldx = _matrix(x, (n, w), x.dtype, "x")
     pg, ldg = _matrix(gate, (n, w), x.dtype, "gate")
@@ -322,7 +334,7 @@ def quantize_weights(h, turned=None, turned_scales=None, codes=None, scales=None
     """Codes of fp32 weights h [n_in, n_out]: turned [n_out, code_ld(n_in)] for the forward product, codes [n_in, code_ld(n_out)] for
     the input gradient; their scales have a row for each 128 rows of codes."""
     import torch
-    n_in, n_out = tuple(h.shape)
+    n_in, n_out = _rows(h, "h")
     _on_device(h, turned, turned_scales, codes, scales)
     ph, ldh = _matrix(h, (n_in, n_out), torch.float32, "h")
     pt, pts = _code_rows(turned, turned_scales, n_out, n_in, -(-n_out // CODE_BLOCK), "turned")
@@ -332,7 +344,7 @@ def quantize_weights(h, turned=None, turned_scales=None, codes=None, scales=None
 
 def scaled_transform(codes, scales, w_codes, w_scales, n_in, c, accumulate=False, act=ACT_IDENTITY, stream=None):
     """c = act((c +) X W): X rows of n_in codes, W the weights whose rows of codes are c's columns."""
-    dt, (n, n_out) = _dtype(c), tuple(c.shape)
+    dt, (n, n_out) = _dtype(c), _rows(c, "c")
     _on_device(codes, scales, w_codes, w_scales, c)
     pc, ldc = _matrix(c, (n, n_out), c.dtype, "c")
     px, pxs = _code_rows(codes, scales, n, n_in, n, "codes")
@@ -349,7 +361,7 @@ def scaled_weight_workspace(n_rows, n_in, n_out) -> int:
 def scaled_bwd_weight(y_codes, y_scales, d_codes, d_scales, dh, accumulate=False, workspace=None, stream=None):
     """dh (+)= Y^T D, dh [n_in, n_out] fp32, from rows of codes of the inputs and of the errors."""
     import torch
-    n, (n_in, n_out) = y_codes.shape[0], tuple(dh.shape)
+    n, (n_in, n_out) = y_codes.shape[0], _rows(dh, "dh")
     _on_device(y_codes, y_scales, d_codes, d_scales, dh, workspace)
     ph, ldh = _matrix(dh, (n_in, n_out), torch.float32, "dh")
     py, pys = _code_rows(y_codes, y_scales, n, n_in, n, "y_codes")
@@ -360,7 +372,7 @@ def scaled_bwd_weight(y_codes, y_scales, d_codes, d_scales, dh, accumulate=False
 
 def rms_norm_fwd(x, gain, eps, residual=None, total=None, y=None, codes=None, scales=None, inv_rms=None, stream=None):
     """u = x + residual, y = u gain / sqrt(mean u^2 + eps); writes what is given of total (u), y, codes with scales, inv_rms."""
-    dt, (n, w) = _dtype(x), tuple(x.shape)
+    dt, (n, w) = _dtype(x), _rows(x, "x")
     _on_device(x, gain, residual, total, y, codes, scales, inv_rms)
     px, ldx = _matrix(x, (n, w), x.dtype, "x")
     pr, ldr = _matrix(residual, (n, w), x.dtype, "residual")
@@ -379,7 +391,7 @@ def rms_norm_workspace(dtype, n_rows, width) -> int:
 
 def rms_norm_bwd(dy, u, gain, inv_rms, dx=None, dgain=None, dtotal=None, accumulate=False, workspace=None, stream=None):
     """dx = gradient of u through the norm (+ dtotal); dgain (+)= the gain's gradient."""
-    dt, (n, w) = _dtype(dy), tuple(dy.shape)
+    dt, (n, w) = _dtype(dy), _rows(dy, "dy")
     _on_device(dy, u, gain, inv_rms, dx, dgain, dtotal, workspace)
     pd, ldd = _matrix(dy, (n, w), dy.dtype, "dy")
     pu, ldu = _matrix(u, (n, w), dy.dtype, "u")

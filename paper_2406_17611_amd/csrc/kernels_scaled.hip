@@ -88,10 +88,27 @@ __device__ __attribute__((aligned(16))) const uint8_t zero_piece[16] = {};
 __device__ __forceinline__ void copy_to_lds(const uint8_t* from, uint8_t* to) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
+// p or q without a branch: a copy under a branch would count for the lanes that take it only.
+__device__ __forceinline__ const uint8_t* either(bool first, const uint8_t* p, const uint8_t* q) {
+    uintptr_t x = first ? reinterpret_cast<uintptr_t>(p) : reinterpret_cast<uintptr_t>(q);
+    asm volatile("" : "+v"(x));
+    return reinterpret_cast<const uint8_t*>(x);
+}
 // This thread's copies and LDS reads are done, then everybody's.
 __device__ __forceinline__ void copies_done() {
     __builtin_amdgcn_s_waitcnt(0x0070);        // vmcnt(0) lgkmcnt(0)
     __syncthreads();
+}
+
+// The same with N of the youngest loads, stores and copies still under way (they end in order).
+template <int N>
+__device__ __forceinline__ void copies_done_but() {
+    static_assert(N < 64, "six bits");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | (N >> 4) << 14);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
 }
 
 // Order of a row's 16-byte pieces in LDS: the 16 rows that a fragment takes meet all eight places of a row's 128 bytes. Rows of X are
@@ -100,8 +117,9 @@ __device__ __forceinline__ int place_x(int row) { return row & 7; }
 template <typename T>
 __device__ __forceinline__ int place_w(int row) { return sizeof(T) == 2 ? (row & 3) | ((row >> 1) & 4) : row & 7; }
 
-// Long reductions: tiles of 16 MI WM rows x 64 WN outputs, a block of 128 of the reduction at a time through LDS, copied there while the
-// block before is multiplied (two buffers).
+// Long reductions over fewer tiles, and what scaled_big_kernel does not take: tiles of 16 MI WM rows x 64 WN outputs, a block of 128 of the
+// reduction at a time through LDS, copied there while the block before is multiplied (two buffers). 128 x 256 where that makes 256
+// tiles, else 128 x 128, two workgroups per compute unit; 128 x 64 for at most 64 outputs.
 template <typename T, int WM, int WN, int MI>
 __global__ __launch_bounds__(64 * WM * WN, 2) void scaled_tile_kernel(ScaledArgs a, int32_t tiles_n, int32_t tiles) {
     constexpr int WAVES = WM * WN, BM = 16 * MI * WM, BN = 64 * WN, NX = BM / 8 / WAVES, NW = BN / 8 / WAVES;
@@ -141,10 +159,10 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void scaled_tile_kernel(ScaledArgs
             for (int h = 0; h < NW; ++h) copy_to_lds(w + at_w[h], lw + (wave * NW + h) * 1024);
         } else {
 #pragma unroll
-            for (int h = 0; h < NX; ++h) copy_to_lds(piece_x < tail ? x + at_x[h] : zero_piece, lx + (wave * NX + h) * 1024);
+            for (int h = 0; h < NX; ++h) copy_to_lds(either(piece_x < tail, x + at_x[h], zero_piece), lx + (wave * NX + h) * 1024);
 #pragma unroll
             for (int h = 0; h < NW; ++h)
-                copy_to_lds(16 * ((lane & 7) ^ place_w<T>((wave * NW + h) * 8 + sub)) < tail ? w + at_w[h] : zero_piece, lw + (wave * NW + h) * 1024);
+                copy_to_lds(either(16 * ((lane & 7) ^ place_w<T>((wave * NW + h) * 8 + sub)) < tail, w + at_w[h], zero_piece), lw + (wave * NW + h) * 1024);
         }
     };
     // the scales of four blocks at a time
@@ -228,6 +246,158 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void scaled_tile_kernel(ScaledArgs
     }
 }
 
+// Long reductions over many tiles, bf16 results: 256 x 256 outputs per workgroup, 128 x 128 per wavefront (one per SIMD, so that a
+// fragment from LDS is used four times), v_mfma_scale_f32_32x32x64_f8f6f4. A workgroup takes tile after tile and never stops in between:
+// a block of 128 of the reduction is copied while the one before is multiplied, also into the next tile, most fragments of the next 64 are
+// read while the second half of the present 64 is multiplied, and the stores of a tile are under way during the next one's first block.
+// The last tiles are moved back to end with the last row and output, so nothing is masked; elements in two tiles are stored twice, the same
+// value. (Hence not where c is added to. Reductions are whole 256: two buffers.)
+// Weight row [q1 h q0 v1 v0] (bits) of a fragment's 32 is output [q1 q0 h v1 v0] of it: accumulators 4 q + v, q = 0, 1 and 2, 3, of a lane are
+// then 8 consecutive outputs.
+// 262,181 x 2048 -> 2048: 1,150 us, 1,910 TFLOP/s, of which 100 are the stores; 131,072 x 8192 -> 2048 2,385 TFLOP/s. Tiles that start anew
+// (scaled_tile_kernel, 8 wavefronts of 128 x 64): 1,305 and 2,036. With all copies of a block in a row 1,310: a wavefront that issues
+// a copy waits until the one before is taken, and issues no product meanwhile. Without copies 900: what bounds it is the L2, 8.5 TB/s.
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+constexpr int kBigTile = 256, kBigBuffer = 2 * kBigTile * BK;
+
+__global__ __launch_bounds__(kThreads, 1) void scaled_big_kernel(ScaledArgs a, int32_t tiles_n, int32_t tiles) {
+    using T = bf16_t;
+    __shared__ __attribute__((aligned(16))) uint8_t b0[kBigBuffer], b1[kBigBuffer];      // (apart: see scaled_tile_kernel)
+    // runs of tiles for the 8 XCDs; the workgroups of an XCD take them in turn, so that those at work together lie side by side
+    const int32_t run = (tiles + 7) / 8, stride = int32_t(gridDim.x >> 3);
+    const int32_t end = min(tiles, (int32_t(blockIdx.x & 7) + 1) * run);
+    int32_t tile = int32_t(blockIdx.x & 7) * run + int32_t(blockIdx.x >> 3);
+    if (tile >= end) return;                            // whole workgroup
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & 31, half = lane >> 5;
+    const int wm = (wave >> 1) * 128, wn = (wave & 1) * 128;
+    const int64_t ld = code_ld(a.n_in), lds = scale_ld(a.n_in);
+    const int32_t blocks = a.n_in / BK;
+    auto first_row = [&](int32_t t) { return min(int64_t(t / tiles_n) * kBigTile, a.n_rows - kBigTile); };
+    auto first_output = [&](int32_t t) { return min(t % tiles_n * kBigTile, a.n_out - kBigTile); };
+
+    // copies, 8 rows by an instruction: piece (lane % 8) of row lane / 8, in the order of place_x
+    int32_t copy_tile = tile, copy_block = 0;
+    const uint8_t* copy_x = a.x + first_row(tile) * ld;
+    const uint8_t* copy_w = a.w + int64_t(first_output(tile)) * ld;
+    const uint32_t at = uint32_t(wave * 64 + (lane >> 3)) * uint32_t(ld) + 16 * ((lane & 7) ^ (lane >> 3));
+    auto copy_x_rows = [&](uint8_t* to, int h) { copy_to_lds(copy_x + h * 8 * ld + at, to + wave * 8192 + h * 1024); };
+    auto copy_w_rows = [&](uint8_t* to, int h) { copy_to_lds(copy_w + h * 8 * ld + at, to + kBigTile * BK + wave * 8192 + h * 1024); };
+    auto copied = [&]() {                               // (behind the last tile: that one again)
+        copy_x += BK, copy_w += BK;
+        if (++copy_block == blocks) {
+            copy_tile = min(copy_tile + stride, end - 1), copy_block = 0;
+            copy_x = a.x + first_row(copy_tile) * ld, copy_w = a.w + int64_t(first_output(copy_tile)) * ld;
+        }
+    };
+    const int row_w = (l & 0x13) | ((l & 4) << 1) | ((l & 8) >> 1);
+    auto fragment = [&](const uint8_t* row, int part, int place) {
+        return joined(*reinterpret_cast<const uint4*>(row + (((4 * part + half) ^ place) << 4)), *reinterpret_cast<const uint4*>(row + (((4 * part + half + 2) ^ place) << 4)));
+    };
+    auto read_w = [&](const uint8_t* b, int part, int i) { return fragment(b + (kBigTile + wn + 32 * i + row_w) * BK, part, row_w & 7); };
+    auto read_x = [&](const uint8_t* b, int part, int j) { return fragment(b + (wm + 32 * j + l) * BK, part, l & 7); };
+    // the scales of four blocks, of the present one on (in the low byte) and of the next four
+    int sx[4], next_sx[4], sw[4], next_sw[4];
+    auto scales = [&](int32_t t, int32_t block) {
+        const uint8_t* const x = a.x_scales + first_row(t) * lds + block;
+        const uint8_t* const w = a.w_scales + block;
+        const int32_t n0 = first_output(t) + wn + row_w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            next_sx[j] = *reinterpret_cast<const int*>(x + uint32_t(wm + 32 * j + l) * uint32_t(lds));
+            next_sw[j] = *reinterpret_cast<const int*>(w + uint32_t((n0 + 32 * j) / kCodeBlock) * uint32_t(lds));
+        }
+    };
+
+    const float least = a.relu ? 0.f : -INFINITY;
+    floatx16 acc[4][4];
+    intx8 w[4], x0[4], x1[4];
+    auto multiply = [&](int i, const intx8 (&x)[4], auto after) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w[i], x[j], acc[i][j], 0, 0, 0, sw[i], 0, sx[j]);
+            asm volatile("" : "+a"(acc[i][j]));         // (here and not further down, where the fragments would have to be kept for it)
+            after(j);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto nothing = [](int) {};
+    // The copies of the block after the next go where this one lay, once everybody has read it: its X behind the products of the last
+    // quarter, its W behind those of the next block's first, one each, so that no product waits for a row of copies to be taken.
+    auto block = [&](int32_t s, uint8_t* from, uint8_t* other) __attribute__((always_inline)) {
+        if ((s & 3) == 0) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sx[j] = next_sx[j], sw[j] = next_sw[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sx[j] = int(uint32_t(sx[j]) >> 8), sw[j] = int(uint32_t(sw[j]) >> 8);
+        }
+        const bool last = s + 1 == blocks;
+        if (last || (s & 3) == 3) scales(last ? min(tile + stride, end - 1) : tile, last ? 0 : s + 1);
+        multiply(0, x0, [&](int j) { copy_w_rows(other, j); });
+        w[2] = read_w(from, 0, 2), w[3] = read_w(from, 0, 3);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(1, x0, [&](int j) { copy_w_rows(other, 4 + j); });
+        copied();
+        w[0] = read_w(from, 1, 0), w[1] = read_w(from, 1, 1);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x1[j] = read_x(from, 1, j);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(2, x0, nothing);
+        multiply(3, x0, nothing);
+        multiply(0, x1, nothing);
+        w[2] = read_w(from, 1, 2), w[3] = read_w(from, 1, 3);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(1, x1, nothing);
+        copies_done_but<0>();                           // the next block's; and everybody has read this one
+        w[0] = read_w(other, 0, 0), w[1] = read_w(other, 0, 1);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x0[j] = read_x(other, 0, j);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(2, x1, [&](int j) { copy_x_rows(from, j); });
+        multiply(3, x1, [&](int j) { copy_x_rows(from, 4 + j); });
+    };
+    scales(tile, 0);
+#pragma unroll
+    for (int h = 0; h < 8; ++h) copy_x_rows(b0, h), copy_w_rows(b0, h);
+    copied();
+#pragma unroll
+    for (int h = 0; h < 8; ++h) copy_x_rows(b1, h);
+    copies_done_but<0>();
+    w[0] = read_w(b0, 0, 0), w[1] = read_w(b0, 0, 1);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x0[j] = read_x(b0, 0, j);
+    for (; tile < end; tile += stride) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j] = floatx16(0.f);
+#pragma clang loop unroll(disable)
+        for (int32_t s = 0; s < blocks; s += 2) {
+            block(s, b0, b1);
+            block(s + 1, b1, b0);
+        }
+        T* c = static_cast<T*>(a.c) + (first_row(tile) + wm + l) * a.ldc + first_output(tile) + wn + 8 * half;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                for (int q = 0; q < 4; q += 2) {
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        v[e] = acc[i][j][4 * q + e];
+                        v[e] = v[e] < least ? least : v[e];               // (NaN stays)
+                    }
+                    RowPiece<T>::store<false>(c, 32 * i + 8 * q, kBigTile, v);
+                }
+                __builtin_amdgcn_sched_barrier(0);      // (not all accumulators at once)
+            }
+            c += 32 * a.ldc;
+        }
+    }
+}
+
 // Short reductions (512 at most): bound by reading X and writing c. A wavefront keeps the weights of 16 NI outputs in registers
 // and the workgroup walks over rows, 16 R WR at a time, which are copied to LDS D - 1 steps ahead. WN wavefronts take the same rows, their
 // other outputs. (NI: 4; 2 where fp32 results take more than 256 columns, whose weights are kept as bf16, twice the registers.)
@@ -239,10 +409,6 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void scaled_tile_kernel(ScaledArgs
 // supply nothing to the matrix instruction.)
 // 2,449,029 x 512 -> 512 bf16: 839 us, 4.5 TB/s (rows requested into registers one step ahead 1,588; 128 x 128 tiles 1,446); 169,343 x 256 -> 256
 // bf16 35 us (51; 41), fp32 61 us (82; 64).
-template <int N>
-__device__ __forceinline__ void copies_done_but() {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
-}
 template <typename T, int KB, int NI, int WN, int R>
 struct RowsLayout {
     static constexpr int WR = kThreads / 64 / WN, ROWS = 16 * R * WR, COPIES = KB * ROWS * BK / 1024 / 4 + 1, STORES = R * NI * 4 / RowPiece<T>::P;
@@ -272,7 +438,7 @@ __global__ __launch_bounds__(kThreads, (RowsLayout<T, KB, NI, WN, R>::D * RowsLa
         for (int h = 0; h < PER_WAVE; ++h) {
             const int q = wave * PER_WAVE + h, kb = q / (ROWS / 8), row = q % (ROWS / 8) * 8 + sub;
             const uint32_t k = kb * kCodeBlock + piece;
-            copy_to_lds(k < ld ? x + (uint32_t(min(row, last)) * ld + k) : zero_piece, to + q * 1024);
+            copy_to_lds(either(k < ld, x + (uint32_t(min(row, last)) * ld + k), zero_piece), to + q * 1024);
         }
         const uint8_t* const sc = a.x_scales + (base + min(lane, last)) * 4;         // (a scale row is 4 bytes: 512 columns at most)
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)sc,
@@ -378,12 +544,13 @@ hipError_t varco_launch_scaled_transform(int dtype, const ScaledArgs& a, hipStre
                                    int32_t(tiles));
             };
             using std::integral_constant;
-            constexpr int kBig = sizeof(T) == 2 ? 8 : 4;
-            const int64_t big = (a.n_rows + 32 * kBig - 1) / (32 * kBig) * ((a.n_out + 255) / 256);
+            const int64_t big_n = (a.n_out + kBigTile - 1) / kBigTile, big = (a.n_rows + kBigTile - 1) / kBigTile * big_n;
             if (a.n_out <= 64)
                 tile(integral_constant<int, 4>{}, integral_constant<int, 1>{}, integral_constant<int, 2>{});
-            else if (big >= 256)
-                tile(integral_constant<int, 2>{}, integral_constant<int, 4>{}, integral_constant<int, kBig>{});
+            else if (sizeof(T) == 2 && big >= 256 && a.n_rows >= kBigTile && a.n_out >= kBigTile && a.n_in % (2 * BK) == 0 && !a.accumulate)
+                hipLaunchKernelGGL(scaled_big_kernel, dim3(256), dim3(kThreads), 0, stream, a, int32_t(big_n), int32_t(big));
+            else if (2 * big >= 256)
+                tile(integral_constant<int, 2>{}, integral_constant<int, 4>{}, integral_constant<int, 4>{});
             else
                 tile(integral_constant<int, 2>{}, integral_constant<int, 2>{}, integral_constant<int, 4>{});
             return;

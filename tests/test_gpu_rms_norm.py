@@ -187,3 +187,40 @@ def test_gradients_against_differences():
         d = torch.zeros_like(gain)
         d[j] = h
         assert abs((risk(u, gain + d) - risk(u, gain - d)) / (2 * h) - float(dgain[j])) < 2e-3
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("w", [48, 75, 512, 1000, 4100])
+def test_more_rows_than_a_launch_takes_at_once(dtype, w):
+    """Rows that repeat with a period give results that repeat, forward and backward; codes too."""
+    period, n = 191, 150_001 if w < 1000 else 40_001
+    at = torch.arange(n, device="cuda") % period
+    base = [_rows(period, w, dtype, w + k) for k in range(3)]
+    x, r, dy = (t[at].contiguous() for t in base)
+    gain = torch.rand(w, device="cuda") + 0.5
+
+    def passes(x, r, dy):
+        total, y, inv = torch.empty_like(x), torch.empty_like(x), torch.empty(x.shape[0], device="cuda")
+        codes, scales = code_buffers(x.shape[0], w)
+        vb.rms_norm_fwd(x, gain, EPS, residual=r, total=total, y=y, codes=codes, scales=scales, inv_rms=inv)
+        dx = torch.empty_like(x)
+        vb.rms_norm_bwd(dy, total, gain, inv, dx, None, dtotal=y)
+        again, again_scales = code_buffers(x.shape[0], w)
+        vb.quantize_rows(x, again, again_scales, gate=r)
+        return total, y, inv, codes, scales, dx, again, again_scales
+
+    for many, few in zip(passes(x, r, dy), passes(*base)):
+        assert torch.equal(many, few[at])
+
+
+def test_rows_beyond_32_bits_of_bytes():
+    n, w = 2_200_001, 1000
+    x = torch.zeros((n, w), device="cuda")
+    x[-3:] = torch.randn(3, w, generator=torch.Generator().manual_seed(5)).cuda()
+    codes, scales = code_buffers(n, w)
+    y = torch.empty_like(x)
+    vb.rms_norm_fwd(x, None, EPS, y=y, codes=codes, scales=scales)
+    want, _ = oc.rms_norm(f64(x[-3:]), 1.0, EPS)
+    assert_within(f64(y[-3:]), want, (INV + 4 * F) * np.abs(want), "y")
+    _check_codes(codes[-3:], scales[-3:], want, w)
+    assert bool((y[:-3] == 0).all()) and bool((codes[:-3] == 0).all())

@@ -157,3 +157,75 @@ def test_sums_are_the_same_every_time():
     for t in out:
         vb.scaled_bwd_weight(*y, *d, t)
     assert torch.equal(out[0], out[1]) and torch.equal(out[0], out[2])
+
+
+def _dropped_few(dtype, x, w):
+    """_dropped of wide products, for a few rows of x at a time."""
+    return 0.0 if dtype == torch.float32 else np.concatenate([_dropped(dtype, x[i:i + 16], w) for i in range(0, x.shape[0], 16)])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,n_in,n_out,act,accumulate", [
+    (60001, 100, 47, vb.ACT_IDENTITY, False), (60001, 256, 256, vb.ACT_RELU, False), (50003, 300, 100, vb.ACT_IDENTITY, True),
+    (40007, 512, 333, vb.ACT_IDENTITY, False), (130003, 16, 8, vb.ACT_IDENTITY, False),                # rows in many steps of a workgroup
+    (8195, 768, 2056, vb.ACT_RELU, False), (33001, 1024, 700, vb.ACT_IDENTITY, False),                 # more tiles than workgroups, moved back at the ends
+    (8195, 640, 2056, vb.ACT_IDENTITY, False), (8195, 768, 2056, vb.ACT_IDENTITY, True), (9000, 1300, 50, vb.ACT_RELU, False)])
+def test_many_rows(dtype, n, n_in, n_out, act, accumulate):
+    """Rows that repeat with a period of 211: every one of the results is compared."""
+    period = 211
+    codes, exps = _coded(period, n_in, n)
+    w, turned, _ = _weights(n_in, n_out, n_out)
+    x = oc.values(codes, exps)
+    at = np.arange(n) % period
+    start = torch.randn(period, n_out, generator=torch.Generator().manual_seed(1)).to(dtype) if accumulate else torch.zeros(period, n_out, dtype=dtype)
+    want, size = f64(start) + x @ w, np.abs(f64(start)) + np.abs(x) @ np.abs(w)
+    if act == vb.ACT_RELU:
+        want = np.maximum(want, 0.0)
+    sums = (n_in + 1) * 2.0 ** -24 * size + _dropped_few(dtype, x, w)
+    bound = torch.from_numpy(sums + STEP[dtype] * (np.abs(want) + sums) + 1e-38).cuda()
+    want = torch.from_numpy(want).cuda()
+    c = start.cuda()[torch.from_numpy(at).cuda()].contiguous() if accumulate else torch.full((n, n_out), float("nan"), dtype=dtype, device="cuda")
+    x8, s8 = upload_codes(codes, exps, n_in)
+    at = torch.from_numpy(at).cuda()
+    vb.scaled_transform(x8[at].contiguous(), s8[at].contiguous(), *turned, n_in, c, accumulate=accumulate, act=act)
+    assert bool(((c.double() - want[at]).abs() <= bound[at]).all())
+
+
+@pytest.mark.parametrize("n,n_in,n_out", [(70001, 256, 256), (33000, 300, 520), (200003, 47, 100), (20011, 513, 600)])
+def test_weight_gradient_over_many_rows(n, n_in, n_out):
+    """Rows that repeat: the sum over them is the one over a period, weighted."""
+    period = 257
+    yc, ye = _coded(period, n_in, 21)
+    dc, de = _coded(period, n_out, 22)
+    count = np.bincount(np.arange(n) % period, minlength=period)[:, None]
+    y, d = oc.values(yc, ye), oc.values(dc, de)
+    want, size = y.T @ (d * count), np.abs(y.T) @ (np.abs(d) * count)
+    at = torch.arange(n, device="cuda") % period
+    (y8, ys), (d8, ds) = upload_codes(yc, ye, n_in), upload_codes(dc, de, n_out)
+    dh = torch.empty((n_in, n_out), device="cuda")
+    vb.scaled_bwd_weight(y8[at].contiguous(), ys[at].contiguous(), d8[at].contiguous(), ds[at].contiguous(), dh)
+    assert_within(f64(dh), want, n * 2.0 ** -24 * size, "dh")
+
+
+def test_rows_beyond_32_bits_of_bytes():
+    """4.6 GB of codes: the last rows are the only ones that are not zero."""
+    n, w, last = 2_250_001, 2048, 77
+    codes, exps = _coded(last, w, 31)
+    x = oc.values(codes, exps)
+    x8 = torch.zeros((n, w), dtype=torch.uint8, device="cuda")
+    s8 = torch.full((n, vb.scale_ld(w)), 127, dtype=torch.uint8, device="cuda")
+    tail, tail_scales = upload_codes(codes, exps, w)
+    x8[-last:], s8[-last:] = tail, tail_scales
+    h, turned, _ = _weights(w, 8, 32)
+    c = torch.full((n, 8), float("nan"), device="cuda")
+    vb.scaled_transform(x8, s8, *turned, w, c)
+    assert bool((c[:-last] == 0).all())
+    assert_within(f64(c[-last:]), x @ h, w * 2.0 ** -24 * (np.abs(x) @ np.abs(h)), "c")
+    dc, de = _coded(last, 16, 33)
+    d = oc.values(dc, de)
+    d8 = torch.zeros((n, 16), dtype=torch.uint8, device="cuda")
+    ds = torch.full((n, 4), 127, dtype=torch.uint8, device="cuda")
+    d8[-last:], ds[-last:] = upload_codes(dc, de, 16)
+    dh = torch.empty((w, 16), device="cuda")
+    vb.scaled_bwd_weight(x8, s8, d8, ds, dh)
+    assert_within(f64(dh), x.T @ d, last * 2.0 ** -24 * (np.abs(x.T) @ np.abs(d)), "dh")
