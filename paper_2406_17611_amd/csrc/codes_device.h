@@ -66,14 +66,15 @@ __device__ __forceinline__ float lanes_max(float x) {
 
 // A row in pieces of 16 bytes of its storage type, converted to fp32, from any address of an element. ANY: of any length; the piece that
 // the last column ends in is loaded from before it, so that it does not leave the row, and moved down; by how much is the same in
-// all lanes. (1,000,000 bf16 rows of 47, norm and codes 91 us; 160 with the last piece by elements.) Else of whole pieces.
+// all lanes. (1,000,000 bf16 rows of 47, norm and codes 91 us; 160 with the last piece by elements.) Else of whole pieces. ONCE: with the hint that
+// the caches need not keep it, where a kernel reads or writes far more than they hold (kernels_clip.hip, kernels_norm.hip have the figures).
 template <typename T>
 struct RowPiece {
     static constexpr int P = 16 / int(sizeof(T));
-    template <bool ANY = true>
+    template <bool ANY = true, bool ONCE = false>
     static __device__ __forceinline__ void load(const T* row, int32_t at, int32_t width, float (&v)[P]) {
         if constexpr (!ANY) {
-            const uint4 u = at < width ? load_16(row + at) : make_uint4(0u, 0u, 0u, 0u);
+            const uint4 u = at < width ? load_16<ONCE>(row + at) : make_uint4(0u, 0u, 0u, 0u);
             convert(u.x, u.y, u.z, u.w, v);
             return;
         }
@@ -82,7 +83,7 @@ struct RowPiece {
             for (int i = 0; i < P; ++i) v[i] = at + i < width ? Elem<T>::load(row + at + i) : 0.f;
             return;
         }
-        const uint4 u = load_16(row + min(at, width - P));
+        const uint4 u = load_16<ONCE>(row + min(at, width - P));
         uint32_t w[4] = {u.x, u.y, u.z, u.w};
         const int by = width % P ? P - width % P : 0;
         if (by) {
@@ -112,12 +113,13 @@ struct RowPiece {
                 v[i] = __uint_as_float(w[i]);
         }
     }
+    template <bool ONCE>
     static __device__ __forceinline__ uint4 load_16(const T* p) {
         typedef uint32_t any4 __attribute__((ext_vector_type(4), aligned(2)));
-        const any4 u = *reinterpret_cast<const any4*>(p);
+        const any4 u = ONCE ? __builtin_nontemporal_load(reinterpret_cast<const any4*>(p)) : *reinterpret_cast<const any4*>(p);
         return make_uint4(u[0], u[1], u[2], u[3]);
     }
-    template <bool ANY = true>
+    template <bool ANY = true, bool ONCE = false>
     static __device__ __forceinline__ void store(T* row, int32_t at, int32_t width, const float (&v)[P]) {
         uint32_t w[4];
 #pragma unroll
@@ -129,7 +131,10 @@ struct RowPiece {
         }
         if (at + P <= width) {
             typedef uint32_t any4 __attribute__((ext_vector_type(4), aligned(2)));
-            *reinterpret_cast<any4*>(row + at) = any4{w[0], w[1], w[2], w[3]};
+            if constexpr (ONCE)
+                __builtin_nontemporal_store(any4{w[0], w[1], w[2], w[3]}, reinterpret_cast<any4*>(row + at));
+            else
+                *reinterpret_cast<any4*>(row + at) = any4{w[0], w[1], w[2], w[3]};
         } else if (ANY && at < width) {                // what is left, by its binary digits (the same in all lanes)
             typedef uint32_t any2 __attribute__((ext_vector_type(2), aligned(2)));
             typedef uint32_t any1 __attribute__((aligned(2)));

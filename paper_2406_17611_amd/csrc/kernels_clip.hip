@@ -3,6 +3,8 @@
 // 1e-13): the multiprocessors have that to spare, the kernels are bound by reading the gradients.
 // Two launches per 128 tensors: sums of squares per workgroup, then each workgroup of the second launch adds those few
 // sums itself, in one order, instead of a third launch that does it once.
+// 403 tensors of 300 million fp32 elements: norm 194 us (6.2 TB/s), clipped copies 669 us, step 879 us (5.4 TB/s; with loads and stores that the
+// caches keep 219, 744, 978). Six matrices of a small network: 10 us, two launches.
 #include <algorithm>
 #include <type_traits>
 
@@ -73,7 +75,7 @@ __global__ __launch_bounds__(kThreads) void square_sums_kernel(TABLE t, double* 
 #pragma unroll 4
             for (int32_t i = threadIdx.x * P; i < n; i += kThreads * P) {
                 float v[P];
-                Row::template load<decltype(any)::value>(p, i, n, v);
+                Row::template load<decltype(any)::value, true>(p, i, n, v);
 #pragma unroll
                 for (int j = 0; j < P; ++j) sum[j & 3] = fma(double(v[j]), double(v[j]), sum[j & 3]);
             }
@@ -122,11 +124,11 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(TABLE t, const double* 
 #pragma unroll 4
             for (int32_t i = threadIdx.x * P; i < n; i += kThreads * P) {
                 float v[P], w[P];
-                Row::template load<ANY>(p, i, n, v);
-                if (STEP) Row::template load<ANY>(q, i, n, w);
+                Row::template load<ANY, true>(p, i, n, v);
+                if (STEP) Row::template load<ANY, true>(q, i, n, w);
 #pragma unroll
                 for (int j = 0; j < P; ++j) v[j] = STEP ? fmaf(-f, v[j], w[j]) : f * v[j];
-                Row::template store<ANY>(q, i, n, v);
+                Row::template store<ANY, true>(q, i, n, v);
             }
         };
         if (n % P)
