@@ -78,6 +78,7 @@ class PartitionedNetwork:
         self._zcap = [0] * self.L
         self._dzcap = [0] * self.L
         self._streams = None
+        self._norm = self._flat_lists = None
         self._capture_stream = None        # one for all captures: each stream has a workspace set of its own
         self._prepared = set()
         self._prepare([None])
@@ -322,8 +323,21 @@ class PartitionedNetwork:
                                   self._row_loss[r], self._row_correct[r], self._totals, stream)
         return self._totals
 
-    def sgd(self, lr: float, stream=None):
+    def sgd(self, lr: float, stream=None, max_norm=None):
+        """The gradient step on all weights. max_norm: with the gradients limited to that norm, all of them together; the device tensor
+        [their norm, the factor that limited them] is returned then."""
         w, dw = self._whole(self._h_flat, self.h1, self.h0), self._whole(self._dh_flat, self.dh1, self.dh0)
+        if max_norm is not None:
+            if self._norm is None:
+                self._norm = torch.empty(2, dtype=torch.float32, device=self.device)
+            if w is not None and dw is not None:
+                if self._flat_lists is None:                 # of the network's own two buffers, which stay
+                    self._flat_lists = vb.TensorList([w]), vb.TensorList([dw])
+                lists = self._flat_lists
+            else:
+                lists = [[h for pair in zip(first, second) for h in pair if h is not None] for first, second in ((self.h1, self.h0), (self.dh1, self.dh0))]
+            vb.sgd_step_clipped(*lists, lr, max_norm, self._norm, stream=stream)
+            return self._norm
         if w is not None and dw is not None:
             return vb.sgd_step(w, dw, lr, stream)
         for l in range(self.L):
@@ -331,13 +345,13 @@ class PartitionedNetwork:
             if self.h0[l] is not None:
                 vb.sgd_step(self.h0[l], self.dh0[l], lr, stream)
 
-    def train_step(self, step: int, ratio, lr: float, stream=None):
-        """Forward with the compressed exchange, loss, backward, summed weight gradients, gradient step."""
+    def train_step(self, step: int, ratio, lr: float, stream=None, max_norm=None):
+        """Forward with the compressed exchange, loss, backward, summed weight gradients, gradient step (max_norm: see sgd)."""
         self.zero_grads()
         self.forward(step, ratio, stream)
         totals = self.loss(True, True, stream)
         self.backward(stream)
-        self.sgd(lr, stream)
+        self.sgd(lr, stream, max_norm)
         return totals
 
     # ------------------------------------------------------------------ HIP graph of one step

@@ -1,12 +1,13 @@
 """Accuracy against communicated bytes on a labelled synthetic graph, for the settings Section V compares:
 full communication, no communication, a fixed compression ratio and the variable schedule (Algorithm 1).
 
-    python -m paper_2406_17611_amd.train_demo [--steps 150] [--blocks 8] [--block-size 2000] [--parts 8]
+    python -m paper_2406_17611_amd.train_demo [--steps 150] [--blocks 8] [--block-size 2000] [--parts 8] [--max-norm N]
 
 The graph is a stochastic block model whose blocks are the classes, dealt to random equal partitions (so most
 neighbours of a node are remote); features carry a weak class signal under unit noise, so that aggregating over
 neighbours, i.e. communicating, matters. Prints one JSON line per setting: held-out accuracy and the bytes
-handed off between partitions (forward + backward) along the run. All arithmetic runs in libvarco's kernels.
+handed off between partitions (forward + backward) along the run; with --max-norm, gradients limited to that norm, the norm
+of the last step's as well. All arithmetic runs in libvarco's kernels.
 """
 from __future__ import annotations
 
@@ -21,7 +22,7 @@ from . import synth
 from .runner import PartitionedNetwork
 
 
-def run(task, name, ratio_of_step, steps, lr, every):
+def run(task, name, ratio_of_step, steps, lr, every, max_norm=None):
     host = vb.partition_build(task.graph.n, task.graph.rowptr, task.graph.colidx, task.graph.vals, task.part, task.n_parts)
     net = PartitionedNetwork(host, task.widths, task.conv, synth.MASK_KEY)
     L = net.L
@@ -37,7 +38,7 @@ def run(task, name, ratio_of_step, steps, lr, every):
     for step in range(steps):
         ratio = ratio_of_step(step)
         before = traffic()
-        totals = net.train_step(step, ratio, lr)
+        totals = net.train_step(step, ratio, lr, max_norm=max_norm)
         sent += traffic() - before               # training traffic only; the evaluation passes below are not counted
         if (step + 1) % every == 0 or step == steps - 1:
             torch.cuda.synchronize()
@@ -46,7 +47,8 @@ def run(task, name, ratio_of_step, steps, lr, every):
             t = net.loss(train=False, with_gradient=False)
             torch.cuda.synchronize()
             curve.append({"step": step + 1, "train_risk": round(risk, 4),
-                          "test_accuracy": round(float(t.cpu()[1]) / net.n_test, 4), "bytes_sent": int(sent)})
+                          "test_accuracy": round(float(t.cpu()[1]) / net.n_test, 4), "bytes_sent": int(sent),
+                          **({} if max_norm is None else {"gradient_norm": round(float(net._norm.cpu()[0]), 5)})})
     return {"setting": name, "final_test_accuracy": curve[-1]["test_accuracy"], "bytes_sent": curve[-1]["bytes_sent"],
             "curve": curve}
 
@@ -59,6 +61,7 @@ def main():
     ap.add_argument("--parts", type=int, default=8)
     ap.add_argument("--lr", type=float, default=0.5)
     ap.add_argument("--c-max", type=int, default=32)
+    ap.add_argument("--max-norm", type=float, default=None)
     args = ap.parse_args()
     assert torch.cuda.is_available(), "train_demo needs a GPU"
     task = synth.labelled_sbm(n_blocks=args.blocks, block_size=args.block_size, p_in=8.0 / args.block_size,
@@ -74,7 +77,7 @@ def main():
         (f"variable: exponential base 2, c_max {args.c_max}", lambda s: vb.schedule_ratio(vb.SCHED_EXPONENTIAL, s, K, args.c_max, 1, 2)),
     ]
     for name, sched in settings:
-        print(json.dumps(run(task, name, sched, args.steps, args.lr, every)), flush=True)
+        print(json.dumps(run(task, name, sched, args.steps, args.lr, every, args.max_norm)), flush=True)
 
 
 if __name__ == "__main__":

@@ -1,0 +1,252 @@
+"""Norm, codes, their products, loss and a limited gradient step together, as a network with normalised rows uses them: against fp64 on
+the same numbers, captured in graphs, on other streams, and through the runner's training step."""
+import numpy as np
+import pytest
+import torch
+
+from codes_common import code_buffers, f64
+from gpu_common import KEY, both_partitions
+from oracle import codes as oc
+from oracle import train as otrain
+from paper_2406_17611_amd import binding as vb
+from paper_2406_17611_amd import synth
+from paper_2406_17611_amd.runner import PartitionedNetwork
+
+pytestmark = pytest.mark.gpu
+
+EPS, LR, LIMIT = 1e-5, 0.1, 0.02
+
+
+class Block:
+    """u = x + r, n = norm(u), z = relu(n W1), logits = z W2, cross-entropy, and all gradients back to u; products of codes."""
+
+    def __init__(self, n, width, hidden, classes, dtype, seed):
+        g = torch.Generator().manual_seed(seed)
+        self.n, self.width, self.hidden, self.classes, self.dtype = n, width, hidden, classes, dtype
+        rows = lambda w: torch.empty((n, w), dtype=dtype, device="cuda")  # noqa: E731
+        self.x, self.r = (torch.randn(n, width, generator=g).to(dtype).cuda() for _ in range(2))
+        self.labels = torch.randint(-1, classes, (n,), generator=g, dtype=torch.int32).cuda()
+        self.weights = [(torch.randn(a, b, generator=g) / a ** 0.5).cuda() for a, b in ((width, hidden), (hidden, classes))]
+        self.gain = (torch.rand(width, generator=g) + 0.5).cuda()
+        self.u, self.inv, self.z, self.logits = rows(width), torch.empty(n, device="cuda"), rows(hidden), rows(classes)
+        self.d_logits, self.dz, self.dn, self.du = rows(classes), rows(hidden), rows(width), rows(width)
+        self.n8, self.z8, self.l8, self.h8 = (code_buffers(n, w) for w in (width, hidden, classes, hidden))
+        self.w8 = [(*code_buffers(b, a, -(-b // 128)), *code_buffers(a, b, -(-a // 128))) for a, b in ((width, hidden), (hidden, classes))]
+        self.dw = [torch.empty_like(w) for w in self.weights] + [torch.empty(width, device="cuda")]
+        self.norm, self.totals = torch.empty(2, device="cuda"), torch.zeros(2, device="cuda")
+        self.row_loss, self.correct = torch.empty(n, device="cuda"), torch.empty(n, dtype=torch.int32, device="cuda")
+        self.ctx = vb.Context([width, hidden, classes], [vb.ACT_RELU, vb.ACT_IDENTITY], vb.CONV_GCN, 1, KEY, vb.BF16 if dtype == torch.bfloat16 else vb.F32)
+        self.scale = 1.0 / max(1, int((self.labels >= 0).sum()))
+
+    def step(self, stream=None):
+        s = dict(stream=stream)
+        vb.rms_norm_fwd(self.x, self.gain, EPS, residual=self.r, total=self.u, codes=self.n8[0], scales=self.n8[1], inv_rms=self.inv, **s)
+        for w, w8 in zip(self.weights, self.w8):
+            vb.quantize_weights(w, *w8, **s)
+        vb.scaled_transform(*self.n8, *self.w8[0][:2], self.width, self.z, act=vb.ACT_RELU, **s)
+        vb.quantize_rows(self.z, *self.z8, **s)
+        vb.scaled_transform(*self.z8, *self.w8[1][:2], self.hidden, self.logits, **s)
+        self.ctx.softmax_xent(self.logits, self.labels, self.classes, self.scale, self.d_logits, self.row_loss, self.correct, None, **s)
+        vb.quantize_rows(self.d_logits, *self.l8, **s)
+        vb.scaled_bwd_weight(*self.z8, *self.l8, self.dw[1], **s)
+        vb.scaled_transform(*self.l8, *self.w8[1][2:], self.classes, self.dz, **s)
+        vb.quantize_rows(self.dz, *self.h8, gate=self.z, **s)
+        vb.scaled_bwd_weight(*self.n8, *self.h8, self.dw[0], **s)
+        vb.scaled_transform(*self.h8, *self.w8[0][2:], self.hidden, self.dn, **s)
+        vb.rms_norm_bwd(self.dn, self.u, self.gain, self.inv, self.du, self.dw[2], **s)
+        vb.sgd_step_clipped(self.weights + [self.gain], self.dw, LR, LIMIT, self.norm, **s)
+
+    def results(self):
+        return [t.clone() for t in (self.u, self.z, self.logits, self.d_logits, self.du, self.norm, *self.dw, *self.weights, self.gain)]
+
+
+def _stored(v, dtype):
+    return v.astype(np.float32).astype(np.float64) if dtype == torch.float32 else f64(torch.from_numpy(v).to(torch.bfloat16))
+
+
+def _reference(b):
+    """The same in fp64, rounded where the device stores."""
+    st = lambda v: _stored(v, b.dtype)  # noqa: E731
+    coded = lambda v: oc.values(*oc.quantize_rows(v))  # noqa: E731
+    w1, w2 = (oc.weight_values(*oc.quantize_weights(f64(w))) for w in b.weights)
+    u = st(f64(b.x) + f64(b.r))
+    y, inv = oc.rms_norm(u, f64(b.gain), EPS)
+    n8 = coded(y)
+    z = st(np.maximum(n8 @ w1, 0.0))
+    z8 = coded(z)
+    logits = st(z8 @ w2)
+    _, d, _ = otrain.softmax_xent(logits, b.labels.cpu().numpy(), b.scale)
+    d = st(d)
+    l8 = coded(d)
+    dz = st(l8 @ w2.T)
+    h8 = coded(np.where(z > 0, dz, 0.0))
+    dn = st(h8 @ w1.T)
+    du, dgain = oc.rms_norm_backward(dn, u, f64(b.gain), inv)
+    dw = [n8.T @ h8, z8.T @ l8, dgain]
+    norm, f = oc.limit(dw, LIMIT)
+    new = [f64(w) - LR * f * g for w, g in zip(b.weights + [b.gain], dw)]
+    return [u, z, logits, d, st(du), np.array([norm, f]), *dw, *new]
+
+
+# Norm-wise. bf16: a result is rounded by 2^-9 of itself at most; where both sides' sums round to different neighbours (2^-8 apart) the codes
+# made of them differ by a step (2^-3) for one in 2^5 of those at most, 2^-3 2^-2.5 2^-2.5 = 2^-8 of the rows' norm. Six roundings and four
+# sets of codes lie between the inputs and du: (6 + 4 2) 2^-9 < 2^-5. fp32: 2^-24 instead of 2^-9, and a share of 2^-20 of the codes
+# differ by a step, 2^-3 2^-10 for each of four sets: below 2^-10.
+@pytest.mark.parametrize("dtype,tol", [(torch.float32, 2.0 ** -10), (torch.bfloat16, 2.0 ** -5)])
+@pytest.mark.parametrize("n,width,hidden,classes", [(700, 100, 256, 47), (333, 256, 130, 8), (1, 64, 32, 5)])
+def test_a_training_step_of_normalised_layers(dtype, tol, n, width, hidden, classes):
+    b = Block(n, width, hidden, classes, dtype, n)
+    want = _reference(b)
+    b.step()
+    for i, (got, ref) in enumerate(zip(b.results(), want)):
+        off, size = np.linalg.norm(f64(got) - ref), np.linalg.norm(ref)
+        assert off <= tol * size + 1e-30, (i, off, size)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_replayed_steps_equal_eager_ones(dtype):
+    """Several replays with other work in between; weights go on changing from replay to replay."""
+    eager, captured = (Block(3000, 100, 256, 47, dtype, 5) for _ in range(2))
+    eager.step()
+    captured.step()
+    want = []
+    for _ in range(4):
+        eager.step()
+        want.append(eager.results())
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    keep = [t.clone() for t in captured.weights + [captured.gain]]
+    with torch.cuda.graph(graph):
+        captured.step()
+    for t, k in zip(captured.weights + [captured.gain], keep):
+        assert torch.equal(t, k)                                       # nothing ran while it was captured
+    junk = torch.zeros(1 << 20, device="cuda")
+    for i in range(4):
+        junk.add_(1.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, ref in zip(captured.results(), want[i]):
+            assert torch.equal(got, ref), i
+    assert float(junk[0]) == 4.0
+
+
+def test_two_graphs_at_a_time():
+    """Captured on one stream, replayed on two: each has scratch memory of its own."""
+    blocks = [Block(20000, 128, 256, 16, torch.bfloat16, 6 + i) for i in range(2)]
+    weights = [[w.clone() for w in b.weights + [b.gain]] for b in blocks]
+
+    def reset(b, ws):
+        for w, k in zip(b.weights + [b.gain], ws):
+            w.copy_(k)
+
+    want = []
+    for b, ws in zip(blocks, weights):
+        b.step()
+        torch.cuda.synchronize()
+        want.append(b.results())
+        reset(b, ws)
+    graphs = []
+    for b in blocks:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            b.step()
+        graphs.append(g)
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for _ in range(5):
+        for b, ws in zip(blocks, weights):
+            reset(b, ws)
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for b, ref in zip(blocks, want):
+            for got, r in zip(b.results(), ref):
+                assert torch.equal(got, r)
+
+
+def test_on_a_stream_that_is_not_the_current_one():
+    a, b = (Block(5000, 100, 200, 40, torch.bfloat16, 9) for _ in range(2))
+    a.step()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    b.step(side)
+    raw = torch.cuda.Stream()
+    raw.wait_stream(side)
+    b.step(raw.cuda_stream)                                            # and as a handle
+    a.step()
+    torch.cuda.synchronize()
+    for x, y in zip(a.results(), b.results()):
+        assert torch.equal(x, y)
+
+
+def test_calls_refuse_what_they_cannot_take():
+    x = torch.zeros(4, 100, device="cuda")
+    codes, scales = code_buffers(4, 100)
+    bad = [
+        lambda: vb.quantize_rows(x.half(), codes, scales), lambda: vb.quantize_rows(x.cpu(), codes, scales),
+        lambda: vb.quantize_rows(x, codes[:, :100], scales), lambda: vb.quantize_rows(x, codes[:3], scales), lambda: vb.quantize_rows(x, codes, None),
+        lambda: vb.quantize_rows(x.t(), codes, scales), lambda: vb.quantize_rows(x, codes, scales, gate=x[:3]),
+        lambda: vb.quantize_rows(x, codes, scales, gate=x.bfloat16()), lambda: vb.quantize_rows(x[0], codes, scales),
+        lambda: vb.quantize_rows(x[:1].expand(4, 100), codes, scales),
+        lambda: vb.rms_norm_fwd(x, torch.ones(99, device="cuda"), 1e-5, y=x), lambda: vb.rms_norm_fwd(x, None, 1e-5),
+        lambda: vb.rms_norm_fwd(x, None, 1e-5, y=x, total=x), lambda: vb.rms_norm_fwd(x, None, -1.0, y=x),
+        lambda: vb.rms_norm_bwd(x, x, None, torch.ones(3, device="cuda"), x), lambda: vb.rms_norm_bwd(x, x, None, torch.ones(4, device="cuda")),
+        lambda: vb.scaled_transform(codes, scales, codes, scales, 100, torch.zeros(4, 5, device="cuda")),
+        lambda: vb.scaled_transform(codes, scales, codes, scales[:1], 200, torch.zeros(4, 4, device="cuda")),
+        lambda: vb.scaled_bwd_weight(codes, scales, codes, scales, torch.zeros(100, 90, device="cuda")),
+        lambda: vb.scaled_bwd_weight(codes, scales, codes, scales, torch.zeros(100, 100, dtype=torch.bfloat16, device="cuda")),
+        lambda: vb.quantize_weights(x), lambda: vb.quantize_weights(x.bfloat16(), codes=codes, scales=scales[:1]),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(vb.VarcoError):
+            call()
+            print(i)
+    big = torch.zeros(200000, 64, device="cuda")
+    with pytest.raises(vb.VarcoError) as e:
+        vb.rms_norm_bwd(big, big, None, torch.ones(200000, device="cuda"), None, torch.zeros(64, device="cuda"), workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+    assert e.value.code == vb.ERR_STATE
+    with pytest.raises(vb.VarcoError):                                 # a scratch tensor that starts between multiples of 256 bytes
+        vb.rms_norm_bwd(big, big, None, torch.ones(200000, device="cuda"), None, torch.zeros(64, device="cuda"), workspace=torch.empty(1 << 20, dtype=torch.uint8, device="cuda")[16:])
+
+
+def _network(dtype="f32"):
+    task = synth.labelled_sbm(n_blocks=4, block_size=150, p_in=0.06, p_out=0.01, width=20, hidden=24, signal=0.4, n_parts=3, conv="sage")
+    host, _ = both_partitions(task.graph, task.part, task.n_parts)
+    net = PartitionedNetwork(host, task.widths, task.conv, KEY, dtype=dtype)
+    net.set_inputs(task.features)
+    net.set_labels(task.labels, task.train)
+    net.set_weights([synth.glorot(task.widths[l], task.widths[l + 1], synth.SEED_WEIGHT, 2 * l) for l in range(net.L)],
+                    [synth.glorot(task.widths[l], task.widths[l + 1], synth.SEED_WEIGHT, 2 * l + 1) for l in range(net.L)])
+    return net
+
+
+@pytest.mark.parametrize("replaced", [False, True])
+@pytest.mark.parametrize("share", [0.25, 4.0])
+def test_training_step_with_limited_gradients(share, replaced):
+    """The runner's step: the weights that a limited step on the gradients it leaves behind gives, whether they are views of one buffer or
+    tensors of their own."""
+    net = _network()
+    if replaced:
+        net.h1[0], net.dh1[0] = net.h1[0].clone(), net.dh1[0].clone()
+    net.train_step(0, (2, 1), 0.0)
+    grads = [g for pair in zip(net.dh1, net.dh0) for g in pair]
+    limit = float(np.float32(oc.limit([f64(g) for g in grads], 1.0)[0] * share))
+    before = [f64(h) for pair in zip(net.h1, net.h0) for h in pair]
+    net.train_step(0, (2, 1), 0.5, max_norm=limit)
+    norm, f = oc.limit([f64(g) for g in grads], limit)
+    got = f64(net._norm)
+    assert abs(got[0] - norm) <= 2.0 ** -23 * norm and abs(got[1] - f) <= 2.0 ** -23 * f
+    for w, b, g in zip([h for pair in zip(net.h1, net.h0) for h in pair], before, grads):
+        d = 0.5 * f * f64(g)
+        assert (np.abs(f64(w) - (b - d)) <= 2.0 ** -24 * np.abs(b - d) + 5 * 2.0 ** -24 * np.abs(d) + 1e-38).all()
+
+
+def test_training_without_a_limit_is_as_it_was():
+    a, b = _network(), _network()
+    for step in range(3):
+        a.train_step(step, (2, 1), 0.3)
+        b.train_step(step, (2, 1), 0.3, max_norm=float("inf"))
+    for x, y in zip(a.h1 + a.h0, b.h1 + b.h0):
+        assert torch.equal(x, y)
