@@ -520,6 +520,8 @@ int32_t varco_scaled_bwd_weight(int64_t n_rows, int32_t n_in, int32_t n_out, con
 /* Root-mean-square norm, with the residual's addition:
  *   u = x + residual, rounded to the storage type (u = x without one)     s = 1 / sqrt(mean of u^2 over the row + eps)
  *   y[j] = u[j] s gain[j]
+ * in fp32, the sum of the squares too: a row with squares that fp32 cannot hold (elements from about 1e19 on) has s = 0, one
+ * of zeros with eps = 0 s infinite and y NaN.
  * residual, gain (fp32, NULL = 1), total, y, codes (with scales), inv_rms may be NULL; what is given is written: total = u, which
  * the backward call reads, y in the storage type, the codes of y (from its fp32 values), inv_rms[row] = s (fp32). total and y may be
  * x or the residual themselves (same leading dimension), not each other. */
@@ -537,12 +539,12 @@ int32_t varco_rms_norm_bwd(int32_t dtype, int64_t n_rows, int32_t width, const v
 
 /* The norm of all gradients together, norm = sqrt(sum of g^2 over all elements of all tensors), summed in fp64 in one order, and the
  * factor that limits it, f = min(1, max_norm / norm) (1 for norm = 0): out[0] = norm, out[1] = f (fp32, device).
- * A NaN among the gradients makes both NaN, an infinity makes the norm infinite and f = 0.
+ * A NaN among the gradients makes both NaN, an infinity makes the norm infinite and f = 0 (1 where max_norm is infinite too).
  *   varco_gradient_norm     norm and factor
  *   varco_clip_gradients    into[t] = f grads[t]; into[t] may be grads[t]
  *   varco_sgd_step_clipped  w[t] -= lr f dw[t], fp32
- * grads, into, w, dw: host arrays of n_tensors device pointers; sizes: host array of element counts (0 is allowed). Tensors
- * that are written must not overlap others. The arrays are read before the call returns. max_norm >= 0, infinity included. */
+ * grads, into, w, dw: host arrays of n_tensors device pointers, 2^20 at most; sizes: host array of element counts (0 is allowed), 2^42
+ * together at most. Tensors that are written must not overlap others. The arrays are read before the call returns. max_norm >= 0, infinity included. */
 int32_t varco_gradient_norm_workspace(int32_t n_tensors, const int64_t* sizes, int64_t* bytes);
 int32_t varco_gradient_norm(int32_t dtype, int32_t n_tensors, const void* const* grads, const int64_t* sizes, float max_norm, void* out,
                             void* workspace, int64_t workspace_bytes, varco_stream stream);

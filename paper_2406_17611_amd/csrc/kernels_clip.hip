@@ -2,9 +2,10 @@
 // Squares are summed in fp64 (a square of an fp32 number is exact there and neither overflows nor vanishes, and 300 million of them keep
 // 1e-13): the multiprocessors have that to spare, the kernels are bound by reading the gradients.
 // Two launches per 128 tensors: sums of squares per workgroup, then each workgroup of the second launch adds those few
-// sums itself, in one order, instead of a third launch that does it once.
-// 403 tensors of 300 million fp32 elements: norm 194 us (6.2 TB/s), clipped copies 669 us, step 879 us (5.4 TB/s; with loads and stores that the
-// caches keep 219, 744, 978). Six matrices of a small network: 10 us, two launches.
+// sums itself, in one order, instead of a third launch that does it once (six matrices of a small network: 10.1 us, 11.5 with it). The sums of
+// several launches are added once (5,000 tensors of 60 million elements, 40,000 sums, clipped copies 849 us, 1,008 without).
+// 403 tensors of 300 million fp32 elements: norm 194 us (6.2 TB/s), clipped copies 664 us, step 874 us (5.4 TB/s; with loads and stores that the
+// caches keep 219, 744, 978).
 #include <algorithm>
 #include <type_traits>
 
@@ -17,6 +18,7 @@ constexpr int kThreads = 256;
 constexpr int kTensors = 128;        // of one launch: their table is a kernel argument (4 KiB at most; 16 tensors, as a network of a few layers has, fill a smaller one)
 constexpr int kFewTensors = 16;
 constexpr int kWorkgroups = 1024;    // that sum the squares of one launch
+constexpr int kOwnSums = 1024;       // partial sums (one launch's) that every workgroup adds itself; more are added once, in a launch of its own
 
 // Tensors are cut into chunks, numbered through the tensors of a launch.
 template <int N>
@@ -103,12 +105,12 @@ __global__ __launch_bounds__(kThreads) void norm_out_kernel(const double* partia
     factor_of(partial, n_partial, max_norm, out);
 }
 
-// STEP: dst -= lr f src (fp32), else dst = f src.
+// STEP: dst -= lr f src (fp32), else dst = f src. n_partial = 0: out holds norm and factor already.
 template <typename T, bool STEP, typename TABLE>
 __global__ __launch_bounds__(kThreads) void scale_kernel(TABLE t, const double* partial, int32_t n_partial, float max_norm, float lr, float* out) {
     using Row = RowPiece<T>;
     constexpr int P = Row::P;
-    float f = factor_of(partial, n_partial, max_norm, blockIdx.x == 0 ? out : nullptr);
+    float f = n_partial ? factor_of(partial, n_partial, max_norm, blockIdx.x == 0 ? out : nullptr) : out[1];
     const bool same = f == 1.f;
     if (STEP) f *= lr;
     const int32_t chunks = t.first[t.tensors];
@@ -182,6 +184,7 @@ hipError_t launch_scale(int32_t n_tensors, const void* const* src, void* const* 
                         float max_norm, float lr, float* out, hipStream_t stream) {
     const int32_t chunk = chunk_of(total_of(n_tensors, sizes));
     hipError_t err = hipSuccess;
+    if (n_partial > kOwnSums) err = varco_launch_norm_out(partial, n_partial, max_norm, out, stream), n_partial = 0;
     over_launches(n_tensors, sizes, chunk, [&](int32_t i, int32_t n, int64_t chunks) {
         with_table(n, [&](auto most) {
             using TABLE = OutTable<decltype(most)::value>;
@@ -192,7 +195,7 @@ hipError_t launch_scale(int32_t n_tensors, const void* const* src, void* const* 
                                n_partial, max_norm, lr, out);
         });
         if (err == hipSuccess) err = hipGetLastError();
-        out = nullptr;
+        if (n_partial) out = nullptr;                    // (written by the first)
     });
     return err;
 }

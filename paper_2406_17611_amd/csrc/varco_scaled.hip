@@ -51,6 +51,7 @@ int32_t check_workspace(const void* workspace, int64_t have, int64_t need, const
 }
 int32_t check_tensors(int32_t n_tensors, std::initializer_list<const void* const*> lists, const int64_t* sizes, uintptr_t bytes, const char* fn) {
     if (n_tensors < 0) return refuse(VARCO_ERR_SHAPE, fn, "negative count of tensors");
+    if (n_tensors > 1 << 20) return refuse(VARCO_ERR_SHAPE, fn, "more than 2^20 tensors");
     if (n_tensors == 0) return VARCO_OK;
     if (!sizes) return refuse(VARCO_ERR_INVALID_ARG, fn, "null array");
     int64_t total = 0;

@@ -91,6 +91,36 @@ def test_not_finite():
     assert torch.isnan(out).all()
 
 
+def test_an_infinite_norm_and_no_limit():
+    g = [torch.ones(100, device="cuda")]
+    g[0][7] = float("inf")
+    out = torch.empty(2, device="cuda")
+    vb.clip_gradients(g, float("inf"), out)
+    assert float(out[0]) == float("inf") and float(out[1]) == 1.0 and int((g[0] == 1).sum()) == 99
+
+
+@pytest.mark.parametrize("sizes", [[40 * 1024] * 300, [i % 7 * 1024 + i % 5 for i in range(3000)]])
+def test_more_tensors_than_a_launch_takes(sizes):
+    """Thousands of partial sums, of several launches."""
+    grads, flat = _tensors(sizes, torch.float32, 5)
+    weights, others = _tensors(sizes, torch.float32, 6)
+    start = others.clone()
+    g = np.zeros(flat.numel())                                         # (the elements between the tensors are of none)
+    for t in grads:
+        g[t.storage_offset():t.storage_offset() + t.numel()] = f64(t)
+    norm, f = oc.limit([g], 1.0)
+    out = torch.empty(2, device="cuda")
+    for _ in range(3):
+        others.copy_(start)
+        vb.sgd_step_clipped(weights, grads, 0.1, 1.0, out)
+        assert_within(f64(out), [norm, f], 2 * F * np.array([norm, f]), "norm and factor")
+        d = np.float64(np.float32(0.1)) * f * g
+        assert_within(f64(others), f64(start) - d, F * np.abs(f64(start) - d) + 5 * F * np.abs(d) + 1e-38, "w")
+    vb.clip_gradients(grads, 1.0, out)
+    for a, w, s in zip(grads, weights, _tensors(sizes, torch.float32, 5)[0]):
+        assert_within(f64(a), f * f64(s), 3 * F * np.abs(f * f64(s)) + 1e-38, "in place")
+
+
 def test_limits_of_nothing_and_everything():
     g = [torch.randn(50, device="cuda")]
     keep = g[0].clone()
