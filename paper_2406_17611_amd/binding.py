@@ -254,13 +254,15 @@ def _dtype(t):
     return code
 
 
-def _on_device(*tensors):
-    """Tensors of a call are on the device that is current (a launch goes there, whatever device the memory is on)."""
+def _on_device(stream, *tensors):
+    """Stream and tensors of a call are of the device that is current (a launch goes to the stream's, whatever device the memory is on)."""
     import torch
     current = torch.cuda.current_device()
     for t in tensors:
         if t is not None and t.get_device() != current:
             _refuse(ERR_INVALID_ARG, f"a tensor on {t.device}, the current device is cuda:{current}")
+    if hasattr(stream, "device_index") and stream.device_index != current:
+        _refuse(ERR_INVALID_ARG, f"a stream of cuda:{stream.device_index}, the current device is cuda:{current}")
 
 
 def _matrix(t, shape, like, what):
@@ -315,15 +317,19 @@ def _scratch(need, workspace, device, stream):
         if stream is None:
             workspace = torch.empty(need, dtype=torch.uint8, device=device)
         else:
-            with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(stream)):
+            if not hasattr(stream, "cuda_stream"):               # a handle; 0 is the default stream's
+                stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+            with torch.cuda.stream(stream):
                 workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    elif not workspace.is_contiguous():
+        _refuse(ERR_SHAPE, "a workspace that is not consecutive in memory")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
 def quantize_rows(x, codes, scales, gate=None, stream=None):
     """codes [n, code_ld(width)], scales [n, scale_ld(width)] of the rows of x (of x where gate > 0)."""
     dt, (n, w) = _dtype(x), _rows(x, "x")
-    _on_device(x, codes, scales, gate)
+    _on_device(stream, x, codes, scales, gate)
     px, ldx = _matrix(x, (n, w), x.dtype, "x")
     pg, ldg = _matrix(gate, (n, w), x.dtype, "gate")
     pc, ps = _code_rows(codes, scales, n, w, n, "codes")
@@ -335,7 +341,7 @@ def quantize_weights(h, turned=None, turned_scales=None, codes=None, scales=None
     the input gradient; their scales have a row for each 128 rows of codes."""
     import torch
     n_in, n_out = _rows(h, "h")
-    _on_device(h, turned, turned_scales, codes, scales)
+    _on_device(stream, h, turned, turned_scales, codes, scales)
     ph, ldh = _matrix(h, (n_in, n_out), torch.float32, "h")
     pt, pts = _code_rows(turned, turned_scales, n_out, n_in, -(-n_out // CODE_BLOCK), "turned")
     pc, ps = _code_rows(codes, scales, n_in, n_out, -(-n_in // CODE_BLOCK), "codes")
@@ -345,7 +351,7 @@ def quantize_weights(h, turned=None, turned_scales=None, codes=None, scales=None
 def scaled_transform(codes, scales, w_codes, w_scales, n_in, c, accumulate=False, act=ACT_IDENTITY, stream=None):
     """c = act((c +) X W): X rows of n_in codes, W the weights whose rows of codes are c's columns."""
     dt, (n, n_out) = _dtype(c), _rows(c, "c")
-    _on_device(codes, scales, w_codes, w_scales, c)
+    _on_device(stream, codes, scales, w_codes, w_scales, c)
     pc, ldc = _matrix(c, (n, n_out), c.dtype, "c")
     px, pxs = _code_rows(codes, scales, n, n_in, n, "codes")
     pw, pws = _code_rows(w_codes, w_scales, n_out, n_in, -(-n_out // CODE_BLOCK), "w_codes")
@@ -362,7 +368,7 @@ def scaled_bwd_weight(y_codes, y_scales, d_codes, d_scales, dh, accumulate=False
     """dh (+)= Y^T D, dh [n_in, n_out] fp32, from rows of codes of the inputs and of the errors."""
     import torch
     n, (n_in, n_out) = y_codes.shape[0], _rows(dh, "dh")
-    _on_device(y_codes, y_scales, d_codes, d_scales, dh, workspace)
+    _on_device(stream, y_codes, y_scales, d_codes, d_scales, dh, workspace)
     ph, ldh = _matrix(dh, (n_in, n_out), torch.float32, "dh")
     py, pys = _code_rows(y_codes, y_scales, n, n_in, n, "y_codes")
     pd, pds = _code_rows(d_codes, d_scales, n, n_out, n, "d_codes")
@@ -373,7 +379,7 @@ def scaled_bwd_weight(y_codes, y_scales, d_codes, d_scales, dh, accumulate=False
 def rms_norm_fwd(x, gain, eps, residual=None, total=None, y=None, codes=None, scales=None, inv_rms=None, stream=None):
     """u = x + residual, y = u gain / sqrt(mean u^2 + eps); writes what is given of total (u), y, codes with scales, inv_rms."""
     dt, (n, w) = _dtype(x), _rows(x, "x")
-    _on_device(x, gain, residual, total, y, codes, scales, inv_rms)
+    _on_device(stream, x, gain, residual, total, y, codes, scales, inv_rms)
     px, ldx = _matrix(x, (n, w), x.dtype, "x")
     pr, ldr = _matrix(residual, (n, w), x.dtype, "residual")
     pt, ldt = _matrix(total, (n, w), x.dtype, "total")
@@ -392,7 +398,7 @@ def rms_norm_workspace(dtype, n_rows, width) -> int:
 def rms_norm_bwd(dy, u, gain, inv_rms, dx=None, dgain=None, dtotal=None, accumulate=False, workspace=None, stream=None):
     """dx = gradient of u through the norm (+ dtotal); dgain (+)= the gain's gradient."""
     dt, (n, w) = _dtype(dy), _rows(dy, "dy")
-    _on_device(dy, u, gain, inv_rms, dx, dgain, dtotal, workspace)
+    _on_device(stream, dy, u, gain, inv_rms, dx, dgain, dtotal, workspace)
     pd, ldd = _matrix(dy, (n, w), dy.dtype, "dy")
     pu, ldu = _matrix(u, (n, w), dy.dtype, "u")
     pt, ldt = _matrix(dtotal, (n, w), dy.dtype, "dtotal")
@@ -453,7 +459,7 @@ def _limit_out(out):
 def gradient_norm(grads, max_norm, out, workspace=None, stream=None):
     """out[0] = norm of all tensors of `grads` together, out[1] = min(1, max_norm / norm)."""
     g = _listed(grads)
-    _on_device(out, workspace, *g.tensors[:1])
+    _on_device(stream, out, workspace, *g.tensors[:1])
     pw, size, held = _scratch(g.need, workspace, out.device, stream)
     _check(lib().varco_gradient_norm(g.dtype, len(g), g.pointers, g.sizes, max_norm, _limit_out(out), pw, size, _stream(stream)))
 
@@ -463,7 +469,7 @@ def clip_gradients(grads, max_norm, out, into=None, workspace=None, stream=None)
     g = _listed(grads)
     to = g if into is None else _listed(into)
     _same_sizes(g, to)
-    _on_device(out, workspace, *g.tensors[:1], *to.tensors[:1])
+    _on_device(stream, out, workspace, *g.tensors[:1], *to.tensors[:1])
     pw, size, held = _scratch(g.need, workspace, out.device, stream)
     _check(lib().varco_clip_gradients(g.dtype, len(g), g.pointers, to.pointers, g.sizes, max_norm, _limit_out(out), pw, size, _stream(stream)))
 
@@ -474,7 +480,7 @@ def sgd_step_clipped(w, dw, lr, max_norm, out, workspace=None, stream=None):
     _same_sizes(g, to)
     if g.dtype != F32:
         _refuse(ERR_UNSUPPORTED, "weights and their gradients are float32")
-    _on_device(out, workspace, *g.tensors[:1], *to.tensors[:1])
+    _on_device(stream, out, workspace, *g.tensors[:1], *to.tensors[:1])
     pw, size, held = _scratch(g.need, workspace, out.device, stream)
     _check(lib().varco_sgd_step_clipped(len(g), to.pointers, g.pointers, g.sizes, lr, max_norm, _limit_out(out), pw, size, _stream(stream)))
 

@@ -426,6 +426,11 @@ class KTapNetwork(PartitionedNetwork):
         for m in mine:                                         # a matrix was replaced by another tensor
             m.zero_()
 
+    def sgd(self, lr: float, stream=None, max_norm=None):
+        if max_norm is not None:                               # (h1, h0 are not what these layers learn)
+            raise ValueError("the limited step of taps is binding.sgd_step_clipped on h and dh")
+        return super().sgd(lr, stream)
+
     def forward(self, step: int, ratio=None, stream=None):
         ctx = self.ctx
         ctx.set_step(step, stream)

@@ -175,6 +175,9 @@ def test_on_a_stream_that_is_not_the_current_one():
     raw = torch.cuda.Stream()
     raw.wait_stream(side)
     b.step(raw.cuda_stream)                                            # and as a handle
+    torch.cuda.default_stream().wait_stream(raw)
+    b.step(0)
+    a.step()
     a.step()
     torch.cuda.synchronize()
     for x, y in zip(a.results(), b.results()):

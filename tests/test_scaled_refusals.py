@@ -3,8 +3,10 @@ before anything is launched, so no device is needed. The pointers are never foll
 import ctypes as C
 
 import pytest
+import torch
 
 from paper_2406_17611_amd import binding as vb
+from paper_2406_17611_amd.runner import KTapNetwork
 
 P, ODD = 0x10000, 0x10001            # addresses, aligned and not
 NAN, INF = float("nan"), float("inf")
@@ -112,7 +114,7 @@ TWO, N = _list(P, P + 400), _sizes(100, 50)
 @pytest.mark.parametrize("change,code,text", [
     (dict(a0=3), vb.ERR_UNSUPPORTED, "dtype"), (dict(a1=-1), vb.ERR_SHAPE, "negative"), (dict(a2=None), vb.ERR_INVALID_ARG, "null array"),
     (dict(a2=_list(P, None)), vb.ERR_INVALID_ARG, "null or at no"), (dict(a2=_list(P, P + 2)), vb.ERR_INVALID_ARG, "null or at no"),
-    (dict(a3=None), vb.ERR_INVALID_ARG, "null array"), (dict(a3=_sizes(1, -1)), vb.ERR_SHAPE, "element count"),
+    (dict(a1=2 ** 20 + 1), vb.ERR_SHAPE, "2^20"), (dict(a3=None), vb.ERR_INVALID_ARG, "null array"), (dict(a3=_sizes(1, -1)), vb.ERR_SHAPE, "element count"),
     (dict(a3=_sizes(1, 2 ** 43)), vb.ERR_SHAPE, "element count"), (dict(a3=_sizes(2 ** 42, 2 ** 42)), vb.ERR_SHAPE, "2^42"),
     (dict(a4=-1.0), vb.ERR_INVALID_ARG, "max_norm"), (dict(a4=NAN), vb.ERR_INVALID_ARG, "max_norm"), (dict(a5=None), vb.ERR_INVALID_ARG, "out"),
     (dict(a7=0), vb.ERR_STATE, "workspace"), (dict(a6=None), vb.ERR_STATE, "workspace"), (dict(a6=P + 8), vb.ERR_INVALID_ARG, "256-byte")])
@@ -166,3 +168,30 @@ def test_norm_workspace(sizes):
                                        ("varco_gradient_norm_workspace", [0, None, None])])
 def test_workspace_queries_refuse_no_output(name, args):
     refused(name, args, vb.ERR_INVALID_ARG, "null output")
+
+
+def test_streams_of_another_device_are_refused(monkeypatch):
+    class Stream:
+        cuda_stream, device_index = 0, 1
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(vb.VarcoError) as e:
+        vb._on_device(Stream())
+    assert e.value.code == vb.ERR_INVALID_ARG
+    Stream.device_index = 0
+    vb._on_device(Stream())
+    vb._on_device(None, None)
+    with pytest.raises(vb.VarcoError):
+        vb._on_device(None, torch.zeros(1))
+
+
+@pytest.mark.parametrize("workspace", [torch.zeros(1, dtype=torch.uint8).expand(4096), torch.zeros(8192, dtype=torch.uint8)[::2]])
+def test_scratch_memory_in_pieces_is_refused(workspace):
+    with pytest.raises(vb.VarcoError) as e:
+        vb._scratch(0, workspace, "cpu", None)
+    assert e.value.code == vb.ERR_SHAPE
+
+
+def test_layers_of_taps_refuse_a_limited_step():
+    """Their weights are not the matrices that the runner's step updates."""
+    with pytest.raises(ValueError):
+        KTapNetwork.sgd(object.__new__(KTapNetwork), 0.1, max_norm=1.0)
