@@ -81,6 +81,74 @@ __device__ __forceinline__ void store_outputs(T* row, int32_t n0, int g, const S
     }
 }
 
+// Values as the 16 bytes of a piece.
+template <typename T>
+__device__ __forceinline__ void pack(const float (&x)[RowPiece<T>::P], uint32_t (&w)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (sizeof(T) == 2)
+            w[j] = bf16_pair(x[2 * j], x[2 * j + 1]);
+        else
+            w[j] = __float_as_uint(x[j]);
+    }
+}
+
+// ONCE: lines that the caches need not keep.
+template <bool ONCE>
+__device__ __forceinline__ void store_16(void* to, const uint32_t (&w)[4]) {
+    typedef uint32_t any4 __attribute__((ext_vector_type(4), aligned(2)));
+    const any4 v = {w[0], w[1], w[2], w[3]};
+    if constexpr (ONCE)
+        __builtin_nontemporal_store(v, static_cast<any4*>(to));
+    else
+        *static_cast<any4*>(to) = v;
+}
+// Of two lanes, one `odd`, that CTRL pairs: the odd one gives its a for the other's b.
+template <int CTRL>
+__device__ __forceinline__ void swap_pieces(bool odd, uint32_t (&a)[4], uint32_t (&b)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t mine = odd ? a[j] : b[j];
+        const uint32_t other = uint32_t(__builtin_amdgcn_update_dpp(int(mine), int(mine), CTRL, 0xF, 0xF, false));
+        a[j] = odd ? other : a[j];
+        b[j] = odd ? b[j] : other;
+    }
+}
+
+// store_outputs for 16 rows where all the wavefront's outputs are there, nothing is added to and rows lie in whole cache lines: lanes l and l + 8
+// of 16 exchange a piece, so that an instruction stores 128 consecutive bytes of 8 rows; the lines need not be kept. c: row 0, `at`: whole_at, rows: from
+// row 0 to the last. (bf16, us, so / by 64 bytes / by 64 bytes and not kept: 169,343 x 256 -> 256 25 / 36 / 31, -> 2048 145 / 245 / 211; 2,449,029 x 512
+// -> 512 805 / 845 / 1,040; 1,000,000 x 200 -> 136, rows that share lines, by 64 bytes 114, not kept 192. fp32 169,343 x 256 -> 256 42 / 54 / 52.)
+template <typename T>
+__device__ __forceinline__ int64_t whole_at(int32_t n0, int g, int l, int64_t ldc) {
+    return (l & 7) * ldc + n0 + output_of<T>(l < 8 ? 0 : RowPiece<T>::P / 4, 4 * g);
+}
+template <typename T, int NI>
+__device__ __forceinline__ void store_whole_outputs(T* c, int64_t at, int64_t rows, int l, const ScaledArgs& a, const floatx4 (&acc)[NI]) {
+    constexpr int P = RowPiece<T>::P, F = P / 4;
+    const int left = int(min(rows, int64_t(16)));
+    c += at;
+#pragma unroll
+    for (int k = 0; k < NI / F; k += 2) {
+        __builtin_amdgcn_sched_barrier(0);             // (not all pieces at once)
+        uint32_t w[2][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float x[P];
+#pragma unroll
+            for (int j = 0; j < P; ++j) {
+                x[j] = acc[F * (k + h) + j / 4][j % 4];
+                if (a.relu) x[j] = x[j] < 0.f ? 0.f : x[j];
+            }
+            pack<T>(x, w[h]);
+        }
+        swap_pieces<0x128>(l >= 8, w[0], w[1]);        // row_ror 8
+        T* const to = c + output_of<T>(F * k, 0);
+        if ((l & 7) < left) store_16<true>(to, w[0]);
+        if ((l & 7) + 8 < left) store_16<true>(to + 8 * a.ldc, w[1]);
+    }
+}
+
 // What the pieces behind the last column of a row are loaded from.
 __device__ __attribute__((aligned(16))) const uint8_t zero_piece[16] = {};
 
@@ -121,7 +189,7 @@ __device__ __forceinline__ int place_w(int row) { return sizeof(T) == 2 ? (row &
 // reduction at a time through LDS, copied there while the block before is multiplied (two buffers). 128 x 256 where that makes 256
 // tiles, else 128 x 128, two workgroups per compute unit; 128 x 64 for at most 64 outputs.
 template <typename T, int WM, int WN, int MI>
-__global__ __launch_bounds__(64 * WM * WN, 2) void scaled_tile_kernel(ScaledArgs a, int32_t tiles_n, int32_t tiles) {
+__global__ __launch_bounds__(64 * WM * WN, 2) void scaled_tile_kernel(ScaledArgs a, int32_t tiles_n, int32_t tiles, bool whole_lines) {
     constexpr int WAVES = WM * WN, BM = 16 * MI * WM, BN = 64 * WN, NX = BM / 8 / WAVES, NW = BN / 8 / WAVES;
     static_assert(NX * 8 * WAVES == BM && NW * 8 * WAVES == BN, "every wavefront copies as many rows");
     __shared__ __attribute__((aligned(16))) uint8_t x0[BM * BK], w0[BN * BK], x1[BM * BK], w1[BN * BK];       // (apart, so that copies to one pair are not taken to alias reads of the other)
@@ -237,12 +305,17 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void scaled_tile_kernel(ScaledArgs
         block(s, x0, w0, x1, w1);
         if (s + 1 < steps) block(s + 1, x1, w1, x0, w0);
     }
+    const int64_t at_c = whole_at<T>(n0 + wn, g, l, a.ldc);
 #pragma unroll
     for (int j = 0; j < MI; ++j) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(acc[j][i]));
-        const int64_t row = m0 + wm + 16 * j + l;
-        if (row < a.n_rows) store_outputs(static_cast<T*>(a.c) + row * a.ldc, n0 + wn, g, a, acc[j]);
+        const int64_t row = m0 + wm + 16 * j;
+        if (whole_lines) {
+            if (n0 + wn < a.n_out) store_whole_outputs(static_cast<T*>(a.c) + row * a.ldc, at_c, a.n_rows - row, l, a, acc[j]);
+        } else if (row + l < a.n_rows) {
+            store_outputs(static_cast<T*>(a.c) + (row + l) * a.ldc, n0 + wn, g, a, acc[j]);
+        }
     }
 }
 
@@ -254,13 +327,13 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void scaled_tile_kernel(ScaledArgs
 // value. (Hence not where c is added to. Reductions are whole 256: two buffers.)
 // Weight row [q1 h q0 v1 v0] (bits) of a fragment's 32 is output [q1 q0 h v1 v0] of it: accumulators 4 q + v, q = 0, 1 and 2, 3, of a lane are
 // then 8 consecutive outputs.
-// 262,181 x 2048 -> 2048: 1,150 us, 1,910 TFLOP/s, of which 100 are the stores; 131,072 x 8192 -> 2048 2,385 TFLOP/s. Tiles that start anew
-// (scaled_tile_kernel, 8 wavefronts of 128 x 64): 1,305 and 2,036. With all copies of a block in a row 1,310: a wavefront that issues
+// 262,181 x 2048 -> 2048: 1,110 us, 1,980 TFLOP/s; 131,072 x 8192 -> 2048 1,805 us, 2,430 TFLOP/s. Tiles that start anew
+// (scaled_tile_kernel, 8 wavefronts of 128 x 64): 1,305 and 2,160. With all copies of a block in a row 1,310: a wavefront that issues
 // a copy waits until the one before is taken, and issues no product meanwhile. Without copies 900: what bounds it is the L2, 8.5 TB/s.
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 constexpr int kBigTile = 256, kBigBuffer = 2 * kBigTile * BK;
 
-__global__ __launch_bounds__(kThreads, 1) void scaled_big_kernel(ScaledArgs a, int32_t tiles_n, int32_t tiles) {
+__global__ __launch_bounds__(kThreads, 1) void scaled_big_kernel(ScaledArgs a, int32_t tiles_n, int32_t tiles, bool whole_lines) {
     using T = bf16_t;
     __shared__ __attribute__((aligned(16))) uint8_t b0[kBigBuffer], b1[kBigBuffer];      // (apart: see scaled_tile_kernel)
     // runs of tiles for the 8 XCDs; the workgroups of an XCD take them in turn, so that those at work together lie side by side
@@ -320,6 +393,41 @@ __global__ __launch_bounds__(kThreads, 1) void scaled_big_kernel(ScaledArgs a, i
             __builtin_amdgcn_sched_barrier(0);
         }
     };
+    // A lane holds four of the eight pieces of 64 outputs of a row, lane + 32 the others; four neighbours exchange them, so that an instruction stores
+    // 128 consecutive bytes of 8 rows. (32 bytes of 32 rows, as the accumulators lie: 16,384 x 4096 -> 4096 257 us, 235 so.)
+    const int64_t c_lane = int64_t(l & ~3) * a.ldc + 16 * (l & 3) + 8 * half;
+    auto store_tile = [&](T* c) __attribute__((always_inline)) {
+        c += c_lane;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+#pragma unroll
+            for (int i = 0; i < 4; i += 2) {
+                uint32_t p[4][4];                           // pieces of the row
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        v[e] = acc[i + (h >> 1)][j][8 * (h & 1) + e];
+                        v[e] = v[e] < least ? least : v[e];               // (NaN stays)
+                    }
+                    pack<T>(v, p[h]);
+                }
+                swap_pieces<0xB1>(l & 1, p[0], p[1]), swap_pieces<0xB1>(l & 1, p[2], p[3]);
+                swap_pieces<0x4E>(l & 2, p[0], p[2]), swap_pieces<0x4E>(l & 2, p[1], p[3]);
+                auto store = [&](auto once) {
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) store_16<decltype(once)::value>(c + 32 * i + h * a.ldc, p[h]);
+                };
+                if (whole_lines)
+                    store(std::true_type{});
+                else
+                    store(std::false_type{});
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            c += 32 * a.ldc;
+        }
+    };
     auto nothing = [](int) {};
     // The copies of the block after the next go where this one lay, once everybody has read it: its X behind the products of the last
     // quarter, its W behind those of the next block's first, one each, so that no product waits for a row of copies to be taken.
@@ -376,25 +484,7 @@ __global__ __launch_bounds__(kThreads, 1) void scaled_big_kernel(ScaledArgs a, i
             block(s, b0, b1);
             block(s + 1, b1, b0);
         }
-        T* c = static_cast<T*>(a.c) + (first_row(tile) + wm + l) * a.ldc + first_output(tile) + wn + 8 * half;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-#pragma unroll
-                for (int q = 0; q < 4; q += 2) {
-                    float v[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        v[e] = acc[i][j][4 * q + e];
-                        v[e] = v[e] < least ? least : v[e];               // (NaN stays)
-                    }
-                    RowPiece<T>::store<false>(c, 32 * i + 8 * q, kBigTile, v);
-                }
-                __builtin_amdgcn_sched_barrier(0);      // (not all accumulators at once)
-            }
-            c += 32 * a.ldc;
-        }
+        store_tile(static_cast<T*>(a.c) + (first_row(tile) + wm) * a.ldc + first_output(tile) + wn);
     }
 }
 
@@ -407,8 +497,8 @@ __global__ __launch_bounds__(kThreads, 1) void scaled_big_kernel(ScaledArgs a, i
 // copies, of the last rows again where there are no more, so that the count holds to the end.
 // (The empty assembly keeps the products in front of the stores' branches: under a branch the lanes that do not take it would
 // supply nothing to the matrix instruction.)
-// 2,449,029 x 512 -> 512 bf16: 839 us, 4.5 TB/s (rows requested into registers one step ahead 1,588; 128 x 128 tiles 1,446); 169,343 x 256 -> 256
-// bf16 35 us (51; 41), fp32 61 us (82; 64).
+// 2,449,029 x 512 -> 512 bf16: 805 us, 4.7 TB/s (rows requested into registers one step ahead 1,588; 128 x 128 tiles 1,446); 169,343 x 256 -> 256
+// bf16 25 us (51; 41), fp32 42 us (82; 64). WHOLE: the rows of c are what store_whole_outputs takes.
 template <typename T, int KB, int NI, int WN, int R>
 struct RowsLayout {
     static constexpr int WR = kThreads / 64 / WN, ROWS = 16 * R * WR, COPIES = KB * ROWS * BK / 1024 / 4 + 1, STORES = R * NI * 4 / RowPiece<T>::P;
@@ -417,7 +507,7 @@ struct RowsLayout {
     static constexpr int BUSY = (D - 2) * COPIES + (D - 1) * STORES;
     static_assert(BUSY < 64 && ROWS <= 64 && KB * ROWS % 32 == 0, "");
 };
-template <typename T, int KB, int NI, int WN, int R>
+template <typename T, int KB, int NI, int WN, int R, bool WHOLE>
 __global__ __launch_bounds__(kThreads, (RowsLayout<T, KB, NI, WN, R>::D * RowsLayout<T, KB, NI, WN, R>::BYTES > 80 * 1024 ? 1 : 2)) void scaled_rows_kernel(ScaledArgs a) {
     using L = RowsLayout<T, KB, NI, WN, R>;
     constexpr int WR = L::WR, ROWS = L::ROWS, D = L::D, PER_WAVE = L::COPIES - 1;
@@ -464,6 +554,7 @@ __global__ __launch_bounds__(kThreads, (RowsLayout<T, KB, NI, WN, R>::D * RowsLa
     const int scale_w = *reinterpret_cast<const int*>(a.w_scales + int64_t(min(n0, a.n_out - 1) / kCodeBlock) * 4);
     const bool regular = n0 + 16 * NI <= a.n_out;
     int filled = 0;                                     // steps that have stored
+    const int64_t at = whole_at<T>(n0, g, l, a.ldc);
 
     auto walk = [&](int64_t r0, const uint8_t* now, uint8_t* next) {
         if (regular && filled >= D - 1)
@@ -503,6 +594,7 @@ __global__ __launch_bounds__(kThreads, (RowsLayout<T, KB, NI, WN, R>::D * RowsLa
                     }
                 }
             }
+            __builtin_amdgcn_sched_barrier(0);
         };
         multiply(std::integral_constant<int, 0>{});
         if constexpr (KB > 1) multiply(std::integral_constant<int, 1>{});
@@ -512,8 +604,15 @@ __global__ __launch_bounds__(kThreads, (RowsLayout<T, KB, NI, WN, R>::D * RowsLa
         for (int r = 0; r < R; ++r) {
 #pragma unroll
             for (int i = 0; i < NI; ++i) asm volatile("" : "+v"(acc[r][i]));
-            const int64_t row = r0 + wr + 16 * r + l;
-            if (row < a.n_rows) store_outputs(static_cast<T*>(a.c) + row * a.ldc, n0, g, a, acc[r]);
+            if constexpr (WHOLE) {
+                __builtin_amdgcn_sched_barrier(0);
+                const int64_t row = r0 + wr + 16 * r;
+                if (regular) store_whole_outputs(static_cast<T*>(a.c) + row * a.ldc, at, a.n_rows - row, l, a, acc[r]);
+                __builtin_amdgcn_sched_barrier(0);
+            } else {
+                const int64_t row = r0 + wr + 16 * r + l;
+                if (row < a.n_rows) store_outputs(static_cast<T*>(a.c) + row * a.ldc, n0, g, a, acc[r]);
+            }
         }
     };
     for (int64_t r0 = first; r0 < a.n_rows;) {
@@ -536,19 +635,20 @@ hipError_t varco_launch_scaled_transform(int dtype, const ScaledArgs& a, hipStre
     auto with_type = [&](auto type) {
         using T = decltype(type);
         const int32_t blocks = (a.n_in + kCodeBlock - 1) / kCodeBlock;
+        const bool whole_lines = !a.accumulate && a.ldc * int64_t(sizeof(T)) % 128 == 0 && reinterpret_cast<uintptr_t>(a.c) % 128 == 0;
         if (blocks > 4) {
             auto tile = [&](auto wm, auto wn, auto mi) {
                 constexpr int WM = decltype(wm)::value, WN = decltype(wn)::value, MI = decltype(mi)::value;
                 const int64_t tiles_n = (a.n_out + 64 * WN - 1) / (64 * WN), tiles = (a.n_rows + 16 * MI * WM - 1) / (16 * MI * WM) * tiles_n;
                 hipLaunchKernelGGL((scaled_tile_kernel<T, WM, WN, MI>), dim3(unsigned((tiles + 7) / 8 * 8)), dim3(64 * WM * WN), 0, stream, a, int32_t(tiles_n),
-                                   int32_t(tiles));
+                                   int32_t(tiles), whole_lines && a.n_out % 64 == 0);
             };
             using std::integral_constant;
             const int64_t big_n = (a.n_out + kBigTile - 1) / kBigTile, big = (a.n_rows + kBigTile - 1) / kBigTile * big_n;
             if (a.n_out <= 64)
                 tile(integral_constant<int, 4>{}, integral_constant<int, 1>{}, integral_constant<int, 2>{});
             else if (sizeof(T) == 2 && big >= 256 && a.n_rows >= kBigTile && a.n_out >= kBigTile && a.n_in % (2 * BK) == 0 && !a.accumulate)
-                hipLaunchKernelGGL(scaled_big_kernel, dim3(256), dim3(kThreads), 0, stream, a, int32_t(big_n), int32_t(big));
+                hipLaunchKernelGGL(scaled_big_kernel, dim3(256), dim3(kThreads), 0, stream, a, int32_t(big_n), int32_t(big), whole_lines && a.n_out % 64 == 0);
             else if (2 * big >= 256)
                 tile(integral_constant<int, 2>{}, integral_constant<int, 4>{}, integral_constant<int, 4>{});
             else
@@ -563,7 +663,11 @@ hipError_t varco_launch_scaled_transform(int dtype, const ScaledArgs& a, hipStre
             // workgroups that are resident together, all columns of the same rows on one XCD (a multiple of 8 in a row of the grid)
             constexpr int kResident = std::max(1, std::min(KB <= 2 && sizeof(T) == 2 ? 3 : 2, 160 * 1024 / (L::D * L::BYTES)));
             const int64_t groups = std::min(steps, std::max<int64_t>(8, 256 * kResident / columns / 8 * 8));
-            hipLaunchKernelGGL((scaled_rows_kernel<T, KB, NI, WN, R>), dim3(unsigned(groups), unsigned(columns)), dim3(kThreads), 0, stream, a);
+            const dim3 grid{unsigned(groups), unsigned(columns)};
+            if (whole_lines && a.n_out % (16 * NI) == 0)
+                hipLaunchKernelGGL((scaled_rows_kernel<T, KB, NI, WN, R, true>), grid, dim3(kThreads), 0, stream, a);
+            else
+                hipLaunchKernelGGL((scaled_rows_kernel<T, KB, NI, WN, R, false>), grid, dim3(kThreads), 0, stream, a);
         };
         auto with_outputs = [&](auto kb) {
             if (a.n_out <= 64)

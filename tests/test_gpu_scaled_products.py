@@ -229,3 +229,23 @@ def test_rows_beyond_32_bits_of_bytes():
     dh = torch.empty((w, 16), device="cuda")
     vb.scaled_bwd_weight(x8, s8, d8, ds, dh)
     assert_within(f64(dh), x.T @ d, last * 2.0 ** -24 * (np.abs(x.T) @ np.abs(d)), "dh")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,n_in,n_out", [(1001, 100, 64), (333, 256, 192), (70, 512, 320), (700, 384, 96), (2049, 768, 128), (300, 520, 576),
+                                          (8200, 768, 2048), (8200, 768, 2112)])
+@pytest.mark.parametrize("gap,lead", [(0, 0), (64, 0), (64, 64), (8, 0), (0, 1), (3, 5)])
+def test_rows_of_results_at_any_place(dtype, n, n_in, n_out, gap, lead):
+    """Rows that fill whole cache lines, with and without others between them, and the same rows elsewhere: the same bits, nothing else."""
+    codes, exps = _coded(211, n_in, n)
+    w, turned, _ = _weights(n_in, n_out, n_out)
+    at = torch.arange(n, device="cuda") % 211
+    x8, s8 = (t[at].contiguous() for t in upload_codes(codes, exps, n_in))
+    want = oc.values(codes, exps) @ w
+    sums = n_in * 2.0 ** -24 * (np.abs(oc.values(codes, exps)) @ np.abs(w)) + _dropped_few(dtype, oc.values(codes, exps), w)
+    bound = torch.from_numpy(sums + STEP[dtype] * (np.abs(want) + sums) + 1e-38).cuda()
+    flat = torch.full((lead + n * (n_out + gap),), float("nan"), dtype=dtype, device="cuda")
+    whole = flat[lead:].view(n, n_out + gap)
+    vb.scaled_transform(x8, s8, *turned, n_in, whole[:, :n_out])
+    assert bool(((whole[:, :n_out].double() - torch.from_numpy(want).cuda()[at]).abs() <= bound[at]).all())
+    assert bool(torch.isnan(whole[:, n_out:]).all()) and bool(torch.isnan(flat[:lead]).all())
