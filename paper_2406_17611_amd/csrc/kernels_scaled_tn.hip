@@ -4,9 +4,10 @@
 // Codes are turned into bf16 on their way into LDS (v_cvt_scalef32_pk_bf16_fp8, which applies the scale), where they lie as in memory, and
 // are transposed when they are read (ds_read_b64_tr_b16 hands lane i of a group of 16 the i-th column of a 4 x 16 block). Row pitch: 64
 // bytes more than a multiple of 256, so that the four rows of such a block start in four different quarters of the banks.
-// The rows are cut into slabs, one workgroup per slab and tile; the slabs' sums are added by a second launch in one order.
-// 2,449,029 rows, 512 x 512: 1,240 us, 1,030 TFLOP/s; bound by the LDS that feeds the matrix units. (Codes requested when they are needed, one
-// buffer, tiles of 128 x 128: 3,260 us.) 169,343 rows, 256 x 256: 51 us, a third of it the partial sums.
+// The rows are cut into slabs, one workgroup per slab and tile, which leaves its sums as they lie in its accumulators; they are added by a second
+// launch in one order. (410,003 rows, 100 x 47: 26 us, 41 with the sums as matrices; 169,343 rows, 256 x 256: 49, 52.)
+// 2,449,029 rows, 512 x 512: 1,250 us, 1,030 TFLOP/s; bound by the LDS that feeds the matrix units. (Codes requested when they are needed, one
+// buffer, tiles of 128 x 128: 3,260 us.) 169,343 rows, 256 x 256: 49 us, half of it the sums of the 256 slabs, 64 MB written and read.
 #include <algorithm>
 
 #include "codes_device.h"
@@ -19,8 +20,6 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef short shortx8 __attribute__((ext_vector_type(8)));
-
-constexpr int kThreads = 256;        // of the sum over slabs
 
 // Sixteen codes as bf16.
 __device__ __forceinline__ void to_bf16(const uint4& q, float scale, uint4 (&out)[2]) {
@@ -81,13 +80,26 @@ struct Slab {
     }
 };
 
-template <int WI, int WJ, int MI, int NJ, int BK>
+template <int WI_, int WJ_, int MI_, int NJ_, int BK>
 struct Tile {
+    static constexpr int WI = WI_, WJ = WJ_, MI = MI_, NJ = NJ_;
     static constexpr int BI = 16 * MI * WI, BJ = 16 * NJ * WJ, THREADS = 64 * WI * WJ, STAGE = BK;
     using Y = Slab<BI, BK, THREADS>;
     using D = Slab<BJ, BK, THREADS>;
     static constexpr int BYTES = 2 * BK * (Y::PITCH + D::PITCH);
 };
+
+// Four elements of a row, added to what it holds if `add`.
+__device__ __forceinline__ void store_four(float* row, int32_t at, int32_t width, floatx4 v, bool add) {
+    float x[4] = {v[0], v[1], v[2], v[3]};
+    if (add) {
+        float c[4];
+        RowPiece<float>::load(row, at, width, c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] += c[i];
+    }
+    RowPiece<float>::store(row, at, width, x);
+}
 
 // Work is numbered slab after slab and dealt to the 8 XCDs in runs, so that the tiles of a slab share its rows in the L2 of one (or two). While a stage is multiplied the next one is
 // on its way to registers; it goes to the other of two buffers when the products have been issued.
@@ -135,57 +147,57 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void scaled_tn_kernel(ScaledWeight
             for (int i = 0; i < MI; ++i) {
                 const bf16x8 fy = fragment<PY>(at_y + buf * kY + h * 32 * PY + i * 32);
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fy, fd[j], acc[i][j], 0, 0, 0);
+                for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fd[j], fy, acc[i][j], 0, 0, 0);
             }
         }
         if (more) y.store(lds + (buf ^ 1u) * kY, r + BK, r1), d.store(lds + 2 * kY + (buf ^ 1u) * kD, r + BK, r1);
         __syncthreads();
     }
-    // accumulator v of a lane is element (4 (lane / 16) + v, lane % 16)
-    float* const out = split > 1 ? a.partial + int64_t(slab) * a.n_in * a.n_out : a.dh;
-    const int64_t ldo = split > 1 ? a.n_out : a.ldh;
-    const bool add = split == 1 && a.accumulate;
+    // accumulator v of a lane is element (lane % 16, 4 (lane / 16) + v)
+    if (split > 1) {
+        // in the order of the accumulators, a kilobyte by an instruction
+        floatx4* const out = reinterpret_cast<floatx4*>(a.partial) + (int64_t(slab) * tiles + tile) * (L::BI * L::BJ / 4) + wave * (MI * NJ * 64) + lane;
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+                if (i0 + wi + 16 * i < a.n_in && j0 + wj + 16 * j < a.n_out) out[(i * NJ + j) * 64] = acc[i][j];
+        return;
+    }
+    const int g = lane >> 4, l = lane & 15;
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const int32_t ri = i0 + wi + 16 * i + 4 * (lane >> 4) + v, cj = j0 + wj + 16 * j + (lane & 15);
-                if (ri < a.n_in && cj < a.n_out) {
-                    float* const p = out + int64_t(ri) * ldo + cj;
-                    *p = add ? *p + acc[i][j][v] : acc[i][j][v];
-                }
-            }
+        for (int j = 0; j < NJ; ++j) {
+            const int32_t ri = i0 + wi + 16 * i + l, cj = j0 + wj + 16 * j + 4 * g;
+            if (ri < a.n_in) store_four(a.dh + ri * a.ldh, cj, a.n_out, acc[i][j], a.accumulate);
+        }
 }
 
-// dh (+)= the slabs' sums: 128 elements per workgroup, eight shares of the slabs, each from its first slab on, then the shares in turn.
+// dh (+)= the slabs' sums, in the order in which the tiles were stored: a fragment of 16 x 16 by 64 threads of four elements, kShares shares of the slabs,
+// each from its first slab on, then the shares in turn.
 constexpr int kShares = 8;
-__global__ __launch_bounds__(kThreads) void slab_sum_kernel(const float* __restrict__ partial, int32_t split, int32_t n_in, int32_t n_out, float* dh,
-                                                            int64_t ldh, int32_t accumulate) {
-    using Row = RowPiece<float>;
-    __shared__ float shares[kShares][128 + 4];
-    const int64_t n = int64_t(n_in) * n_out, e = int64_t(blockIdx.x) * 128;
-    const int lane = threadIdx.x & 31, share = threadIdx.x >> 5;
-    const int32_t here = int32_t(min(int64_t(128), n - e));
-    float x[4] = {0.f, 0.f, 0.f, 0.f};
+template <typename L>
+__global__ __launch_bounds__(64 * kShares) void slab_sum_kernel(const float* __restrict__ partial, int32_t split, int32_t tiles_j, int32_t tiles, int32_t n_in, int32_t n_out,
+                                                                float* dh, int64_t ldh, int32_t accumulate) {
+    __shared__ floatx4 shares[kShares][64];
+    const int lane = threadIdx.x & 63, share = threadIdx.x >> 6;
+    const int32_t tile = int32_t(blockIdx.y), f = int32_t(blockIdx.x);           // fragment of the tile
+    const int32_t wave = f / (L::MI * L::NJ), i = f % (L::MI * L::NJ) / L::NJ, j = f % L::NJ;
+    const int32_t r0 = tile / tiles_j * L::BI + wave / L::WJ * (16 * L::MI) + 16 * i, c0 = tile % tiles_j * L::BJ + wave % L::WJ * (16 * L::NJ) + 16 * j;
+    if (r0 >= n_in || c0 >= n_out) return;              // whole workgroup
+    const floatx4* const from = reinterpret_cast<const floatx4*>(partial) + int64_t(tile) * (L::BI * L::BJ / 4) + f * 64 + lane;
+    const int64_t step = int64_t(tiles) * (L::BI * L::BJ / 4);
+    floatx4 x = floatx4(0.f);
 #pragma unroll 8
-    for (int32_t s = share; s < split; s += kShares) {
-        float v[4];
-        Row::load(partial + s * n + e, 4 * lane, here, v);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] += v[i];
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) shares[share][4 * lane + i] = x[i];
+    for (int32_t s = share; s < split; s += kShares) x += from[s * step];
+    shares[share][lane] = x;
     __syncthreads();
-    if (int(threadIdx.x) >= here) return;
-    float sum = 0.f;
+    if (share) return;
 #pragma unroll
-    for (int i = 0; i < kShares; ++i) sum += shares[i][threadIdx.x];
-    const int64_t at = e + threadIdx.x, row = at / n_out;
-    float* const p = dh + row * ldh + (at - row * n_out);
-    *p = accumulate ? *p + sum : sum;
+    for (int i = 1; i < kShares; ++i) x += shares[i][lane];
+    const int32_t ri = r0 + (lane & 15);
+    if (ri < n_in) store_four(dh + ri * ldh, c0 + 4 * (lane >> 4), n_out, x, accumulate);
 }
 
 template <int WI, int WJ, int MI, int NJ, int BK>
@@ -196,7 +208,7 @@ void launch(Tile<WI, WJ, MI, NJ, BK>, const ScaledWeightArgs& a, int32_t split, 
 
 // Tiles of 256 x 256 where the weights have more than 128 rows and columns and a workgroup per compute unit gets 512 rows or more; else
 // 128 x 128, and 64 on a side of at most 64. (512 x 512 weights, tiles of 256 / of 128: 20,000 rows, 313 each, 36.9 / 30.8 us; 169,343 rows, 2,646 each,
-// 114 / 168; 256 x 256 over 169,343 rows, 661 each, 50.8 / 58.4.)
+// 114 / 168; 256 x 256 over 169,343 rows, 661 each, 49.5 / 58; tiles of 128 x 256, half the sums, there 47.9, over 410,003 rows 93, 87 so.)
 using Big = Tile<2, 4, 8, 4, 64>;
 using Middle = Tile<2, 2, 4, 4, 32>;
 using Narrow = Tile<2, 2, 4, 2, 64>;
@@ -221,30 +233,33 @@ void with_tile(int64_t n_rows, int32_t n_in, int32_t n_out, F f) {
 template <typename L>
 int64_t tiles_of(int32_t n_in, int32_t n_out) { return int64_t((n_in + L::BI - 1) / L::BI) * ((n_out + L::BJ - 1) / L::BJ); }
 int64_t slab_rows(int64_t n_rows, int64_t split, int64_t stage) { return std::max<int64_t>(1, ((n_rows + split - 1) / split + stage - 1) / stage) * stage; }
+template <typename L>
+int32_t split_of(int64_t n_rows, int32_t n_in, int32_t n_out, int64_t wanted) {
+    const int64_t rows = slab_rows(n_rows, std::max<int64_t>(1, std::min<int64_t>(wanted / tiles_of<L>(n_in, n_out), n_rows / 256)), L::STAGE);
+    return int32_t(std::max<int64_t>(1, (n_rows + rows - 1) / rows));
+}
 
 }  // namespace
 
-int32_t varco_scaled_weight_split(int64_t n_rows, int32_t n_in, int32_t n_out) {
-    int64_t split = 1;
+int64_t varco_scaled_weight_floats(int64_t n_rows, int32_t n_in, int32_t n_out) {
+    int64_t floats = 0;
     with_tile(n_rows, n_in, n_out, [&](auto tile, int64_t wanted) {
         using L = decltype(tile);
-        split = std::max<int64_t>(1, std::min<int64_t>(wanted / tiles_of<L>(n_in, n_out), n_rows / 256));
-        const int64_t rows = slab_rows(n_rows, split, L::STAGE);
-        split = std::max<int64_t>(1, (n_rows + rows - 1) / rows);
+        const int64_t split = split_of<L>(n_rows, n_in, n_out, wanted);
+        floats = split > 1 ? split * tiles_of<L>(n_in, n_out) * (L::BI * L::BJ) : 0;
     });
-    return int32_t(split);
+    return floats;
 }
 
 hipError_t varco_launch_scaled_bwd_weight(const ScaledWeightArgs& a, hipStream_t stream) {
-    const int32_t split = varco_scaled_weight_split(a.n_rows, a.n_in, a.n_out);
-    with_tile(a.n_rows, a.n_in, a.n_out, [&](auto tile, int64_t) {
+    with_tile(a.n_rows, a.n_in, a.n_out, [&](auto tile, int64_t wanted) {
         using L = decltype(tile);
-        launch(L{}, a, split, slab_rows(a.n_rows, split, L::STAGE), int32_t((a.n_out + L::BJ - 1) / L::BJ), int32_t(tiles_of<L>(a.n_in, a.n_out)), stream);
+        const int32_t split = split_of<L>(a.n_rows, a.n_in, a.n_out, wanted);
+        const int32_t tiles_j = int32_t((a.n_out + L::BJ - 1) / L::BJ), tiles = int32_t(tiles_of<L>(a.n_in, a.n_out));
+        launch(L{}, a, split, slab_rows(a.n_rows, split, L::STAGE), tiles_j, tiles, stream);
+        if (split > 1)
+            hipLaunchKernelGGL(slab_sum_kernel<L>, dim3(L::BI * L::BJ / 256, tiles), dim3(64 * kShares), 0, stream, a.partial, split, tiles_j, tiles, a.n_in,
+                               a.n_out, a.dh, a.ldh, a.accumulate);
     });
-    if (split > 1) {
-        const int64_t n = int64_t(a.n_in) * a.n_out;
-        hipLaunchKernelGGL(slab_sum_kernel, dim3(unsigned((n + 127) / 128)), dim3(kThreads), 0, stream, a.partial, split,
-                           a.n_in, a.n_out, a.dh, a.ldh, a.accumulate);
-    }
     return hipGetLastError();
 }

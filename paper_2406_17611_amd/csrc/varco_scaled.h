@@ -74,9 +74,9 @@ struct ScaledWeightArgs {
     float* dh;
     int64_t ldh;
     int32_t accumulate;
-    float* partial;               // varco_scaled_weight_split(..) x n_in x n_out floats where that is above 1
+    float* partial;               // varco_scaled_weight_floats(..)
 };
-int32_t varco_scaled_weight_split(int64_t n_rows, int32_t n_in, int32_t n_out);
+int64_t varco_scaled_weight_floats(int64_t n_rows, int32_t n_in, int32_t n_out);
 hipError_t varco_launch_scaled_bwd_weight(const ScaledWeightArgs& a, hipStream_t stream);
 
 // Sum of the squares of all elements in fp64: `blocks` partial sums, then norm and factor in out[0], out[1] by whoever reads them.

@@ -76,11 +76,6 @@ int64_t norm_bytes(int32_t dtype, int64_t n_rows, int32_t width) {
     const int32_t blocks = varco_norm_blocks(dtype, n_rows, width);
     return blocks > 1 ? int64_t(blocks) * width * 4 : 0;
 }
-int64_t weight_bytes(int64_t n_rows, int32_t n_in, int32_t n_out) {
-    const int32_t split = varco_scaled_weight_split(n_rows, n_in, n_out);
-    return split > 1 ? int64_t(split) * n_in * n_out * 4 : 0;
-}
-
 }  // namespace
 
 #define VARCO_CHECK(call)            \
@@ -142,7 +137,7 @@ extern "C" int32_t varco_scaled_weight_workspace(int64_t n_rows, int32_t n_in, i
     VARCO_CHECK(check_rows(n_rows, fn));
     VARCO_CHECK(check_width(n_in, fn));
     VARCO_CHECK(check_width(n_out, fn));
-    *bytes = weight_bytes(n_rows, n_in, n_out);
+    *bytes = varco_scaled_weight_floats(n_rows, n_in, n_out) * 4;
     return VARCO_OK;
 }
 
@@ -158,7 +153,7 @@ extern "C" int32_t varco_scaled_bwd_weight(int64_t n_rows, int32_t n_in, int32_t
         VARCO_CHECK(check_codes(y_codes, y_scales, true, fn));
         VARCO_CHECK(check_codes(d_codes, d_scales, true, fn));
     }
-    VARCO_CHECK(check_workspace(workspace, workspace_bytes, weight_bytes(n_rows, n_in, n_out), fn));
+    VARCO_CHECK(check_workspace(workspace, workspace_bytes, varco_scaled_weight_floats(n_rows, n_in, n_out) * 4, fn));
     ScaledWeightArgs a;
     a.n_rows = n_rows, a.n_in = n_in, a.n_out = n_out;
     a.y = static_cast<const uint8_t*>(y_codes), a.y_scales = static_cast<const uint8_t*>(y_scales);
