@@ -6,8 +6,10 @@
 // bytes more than a multiple of 256, so that the four rows of such a block start in four different quarters of the banks.
 // The rows are cut into slabs, one workgroup per slab and tile, which leaves its sums as they lie in its accumulators; they are added by a second
 // launch in one order. (410,003 rows, 100 x 47: 26 us, 41 with the sums as matrices; 169,343 rows, 256 x 256: 49, 52.)
-// 2,449,029 rows, 512 x 512: 1,250 us, 1,030 TFLOP/s; bound by the LDS that feeds the matrix units. (Codes requested when they are needed, one
-// buffer, tiles of 128 x 128: 3,260 us.) 169,343 rows, 256 x 256: 49 us, half of it the sums of the 256 slabs, 64 MB written and read.
+// 2,449,029 rows, 512 x 512: 1,240 us, 1,040 TFLOP/s: the matrix units work 44 % of the time, the vector ALU (conversion, addresses) a third, and the
+// two wavefronts of a SIMD do the one and the other mostly at the same time. (Codes requested when they are needed, one buffer, tiles of 128 x 128: 3,260 us.
+// LDS layouts without the bank conflicts, a quarter of the cycles: 1,260 to 1,280; conversion between the products: 1,235, and 3 % slower over 256 x 256.)
+// 169,343 rows, 256 x 256: 49 us, half of it the sums of the 256 slabs, 64 MB written and read.
 #include <algorithm>
 
 #include "codes_device.h"
@@ -47,33 +49,37 @@ template <int W, int BK, int THREADS>
 struct Slab {
     static constexpr int PER_ROW = W / 16, N = PER_ROW * BK / THREADS, ROWS = THREADS / PER_ROW, PITCH = W * 2 + 64;
     static_assert(N * THREADS == PER_ROW * BK && ROWS * PER_ROW == THREADS, "every thread takes as many pieces, of the same columns");
-    const uint8_t* codes;
+    const uint8_t* codes;                              // this thread's first piece of the next stage, and its scale
     const uint8_t* scales;
     int64_t ld, lds;
-    bool inside;
+    int first;                                         // its row in a stage
     uint4 q[N];
     uint32_t s[N];
-    __device__ __forceinline__ void start(const uint8_t* c, const uint8_t* sc, int32_t width, int32_t c0) {
+    // (pieces behind the last column repeat the one before; what comes of them is not stored)
+    __device__ __forceinline__ void start(const uint8_t* c, const uint8_t* sc, int32_t width, int32_t c0, int64_t r0) {
         const int32_t col = c0 + 16 * int32_t(threadIdx.x % PER_ROW);
-        ld = code_ld(width), lds = scale_ld(width);
-        inside = col < ld;                             // (a piece is whole or not there)
-        codes = c + min(int64_t(col), ld - 16), scales = sc + min(col, width - 1) / kCodeBlock;
+        ld = code_ld(width), lds = scale_ld(width), first = int(threadIdx.x / PER_ROW);
+        codes = c + (r0 + first) * ld + min(int64_t(col), ld - 16), scales = sc + (r0 + first) * lds + min(col, width - 1) / kCodeBlock;
     }
-    // rows r .. r + BK - 1; those from `end` on are repeated ones until they are stored
-    __device__ __forceinline__ void load(int64_t r, int64_t end) {
+    // a stage of `left` rows: those that there are not are the last one again
+    __device__ __forceinline__ void load(int64_t left) {
+        const int last = int(min(left, int64_t(BK))) - 1 - first;
 #pragma unroll
         for (int h = 0; h < N; ++h) {
-            const int64_t row = min(r + int32_t(threadIdx.x / PER_ROW) + h * ROWS, end - 1);
-            q[h] = *reinterpret_cast<const uint4*>(codes + row * ld);
-            s[h] = scales[row * lds];
+            const int row = min(h * ROWS, last);
+            q[h] = *reinterpret_cast<const uint4*>(codes + __mul24(row, int(ld)));
+            s[h] = scales[__mul24(row, int(lds))];
         }
+        codes += BK * ld, scales += BK * lds;
     }
-    __device__ __forceinline__ void store(uint8_t* to, int64_t r, int64_t end) const {
+    // ... and zeros in one of the operands
+    template <bool ZEROS>
+    __device__ __forceinline__ void store(uint8_t* to, int64_t left) const {
 #pragma unroll
         for (int h = 0; h < N; ++h) {
-            const int32_t row = int32_t(threadIdx.x / PER_ROW) + h * ROWS;
+            const int row = first + h * ROWS;
             uint4 out[2];
-            to_bf16(inside && r + row < end ? q[h] : make_uint4(0u, 0u, 0u, 0u), __uint_as_float(s[h] ? s[h] << 23 : 0x400000u), out);
+            to_bf16(!ZEROS || row < left ? q[h] : make_uint4(0u, 0u, 0u, 0u), __uint_as_float(s[h] ? s[h] << 23 : 0x400000u), out);
             uint4* const p = reinterpret_cast<uint4*>(to + row * PITCH + (threadIdx.x % PER_ROW) * 32);
             p[0] = out[0], p[1] = out[1];
         }
@@ -127,17 +133,17 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void scaled_tn_kernel(ScaledWeight
 
     typename L::Y y;
     typename L::D d;
-    y.start(a.y, a.y_scales, a.n_in, i0);
-    d.start(a.d, a.d_scales, a.n_out, j0);
+    y.start(a.y, a.y_scales, a.n_in, i0, r0);
+    d.start(a.d, a.d_scales, a.n_out, j0, r0);
     if (r0 < r1) {
-        y.load(r0, r1), d.load(r0, r1);
-        y.store(lds, r0, r1), d.store(lds + 2 * kY, r0, r1);
+        y.load(r1 - r0), d.load(r1 - r0);
+        y.template store<false>(lds, r1 - r0), d.template store<true>(lds + 2 * kY, r1 - r0);
     }
     __syncthreads();
     uint32_t buf = 0;
     for (int64_t r = r0; r < r1; r += BK, buf ^= 1u) {
-        const bool more = r + BK < r1;
-        if (more) y.load(r + BK, r1), d.load(r + BK, r1);
+        const int64_t left = r1 - r - BK;
+        if (left > 0) y.load(left), d.load(left);
 #pragma unroll
         for (int h = 0; h < BK / 32; ++h) {
             bf16x8 fd[NJ];
@@ -150,7 +156,7 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void scaled_tn_kernel(ScaledWeight
                 for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fd[j], fy, acc[i][j], 0, 0, 0);
             }
         }
-        if (more) y.store(lds + (buf ^ 1u) * kY, r + BK, r1), d.store(lds + 2 * kY + (buf ^ 1u) * kD, r + BK, r1);
+        if (left > 0) y.template store<false>(lds + (buf ^ 1u) * kY, left), d.template store<true>(lds + 2 * kY + (buf ^ 1u) * kD, left);
         __syncthreads();
     }
     // accumulator v of a lane is element (lane % 16, 4 (lane / 16) + v)
