@@ -242,12 +242,22 @@ def _refuse(code, text):
 
 
 _DTYPES = {}
+_torch = _device = _handle = None
+
+
+def _load_torch():
+    """torch, looked up once: an import statement and two device queries are a fifth of what a small call takes on the host."""
+    global _torch, _device, _handle
+    import torch
+    _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    _handle = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    _DTYPES.update({torch.float32: F32, torch.bfloat16: BF16})
+    _torch = torch
 
 
 def _dtype(t):
-    if not _DTYPES:
-        import torch
-        _DTYPES.update({torch.float32: F32, torch.bfloat16: BF16})
+    if _torch is None:
+        _load_torch()
     code = _DTYPES.get(t.dtype)
     if code is None:
         _refuse(ERR_UNSUPPORTED, f"{t.dtype}: neither float32 nor bfloat16")
@@ -255,14 +265,19 @@ def _dtype(t):
 
 
 def _on_device(stream, *tensors):
-    """Stream and tensors of a call are of the device that is current (a launch goes to the stream's, whatever device the memory is on)."""
-    import torch
-    current = torch.cuda.current_device()
+    """The handle of a call's stream. Stream and tensors are of the device that is current (a launch goes to the stream's, whatever device
+    the memory is on)."""
+    if _torch is None:
+        _load_torch()
+    current = _device()
     for t in tensors:
         if t is not None and t.get_device() != current:
             _refuse(ERR_INVALID_ARG, f"a tensor on {t.device}, the current device is cuda:{current}")
-    if hasattr(stream, "device_index") and stream.device_index != current:
+    if stream is None and _handle is not None:
+        return _handle(current)
+    if getattr(stream, "device_index", current) != current:
         _refuse(ERR_INVALID_ARG, f"a stream of cuda:{stream.device_index}, the current device is cuda:{current}")
+    return _stream(stream)
 
 
 def _matrix(t, shape, like, what):
@@ -287,10 +302,9 @@ def _rows(t, what):
 
 
 def _vector(t, n, what):
-    import torch
     if t is None:
         return None
-    if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous():
+    if t.dtype != _torch.float32 or t.numel() != n or not t.is_contiguous():
         _refuse(ERR_SHAPE, f"{what}: {n} consecutive float32 values are needed")
     return t.data_ptr()
 
@@ -313,14 +327,13 @@ def _scratch(need, workspace, device, stream):
     if workspace is None:
         if need == 0:
             return None, 0, None
-        import torch
         if stream is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=device)
+            workspace = _torch.empty(need, dtype=_torch.uint8, device=device)
         else:
             if not hasattr(stream, "cuda_stream"):               # a handle; 0 is the default stream's
-                stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
-            with torch.cuda.stream(stream):
-                workspace = torch.empty(need, dtype=torch.uint8, device=device)
+                stream = _torch.cuda.ExternalStream(stream) if stream else _torch.cuda.default_stream()
+            with _torch.cuda.stream(stream):
+                workspace = _torch.empty(need, dtype=_torch.uint8, device=device)
     elif not workspace.is_contiguous():
         _refuse(ERR_SHAPE, "a workspace that is not consecutive in memory")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
@@ -329,33 +342,32 @@ def _scratch(need, workspace, device, stream):
 def quantize_rows(x, codes, scales, gate=None, stream=None):
     """codes [n, code_ld(width)], scales [n, scale_ld(width)] of the rows of x (of x where gate > 0)."""
     dt, (n, w) = _dtype(x), _rows(x, "x")
-    _on_device(stream, x, codes, scales, gate)
+    at = _on_device(stream, x, codes, scales, gate)
     px, ldx = _matrix(x, (n, w), x.dtype, "x")
     pg, ldg = _matrix(gate, (n, w), x.dtype, "gate")
     pc, ps = _code_rows(codes, scales, n, w, n, "codes")
-    _check(lib().varco_quantize_rows(dt, n, w, px, ldx, pg, ldg, pc, ps, _stream(stream)))
+    _check(lib().varco_quantize_rows(dt, n, w, px, ldx, pg, ldg, pc, ps, at))
 
 
 def quantize_weights(h, turned=None, turned_scales=None, codes=None, scales=None, stream=None):
     """Codes of fp32 weights h [n_in, n_out]: turned [n_out, code_ld(n_in)] for the forward product, codes [n_in, code_ld(n_out)] for
     the input gradient; their scales have a row for each 128 rows of codes."""
-    import torch
     n_in, n_out = _rows(h, "h")
-    _on_device(stream, h, turned, turned_scales, codes, scales)
-    ph, ldh = _matrix(h, (n_in, n_out), torch.float32, "h")
+    at = _on_device(stream, h, turned, turned_scales, codes, scales)
+    ph, ldh = _matrix(h, (n_in, n_out), _torch.float32, "h")
     pt, pts = _code_rows(turned, turned_scales, n_out, n_in, -(-n_out // CODE_BLOCK), "turned")
     pc, ps = _code_rows(codes, scales, n_in, n_out, -(-n_in // CODE_BLOCK), "codes")
-    _check(lib().varco_quantize_weights(n_in, n_out, ph, ldh, pt, pts, pc, ps, _stream(stream)))
+    _check(lib().varco_quantize_weights(n_in, n_out, ph, ldh, pt, pts, pc, ps, at))
 
 
 def scaled_transform(codes, scales, w_codes, w_scales, n_in, c, accumulate=False, act=ACT_IDENTITY, stream=None):
     """c = act((c +) X W): X rows of n_in codes, W the weights whose rows of codes are c's columns."""
     dt, (n, n_out) = _dtype(c), _rows(c, "c")
-    _on_device(stream, codes, scales, w_codes, w_scales, c)
+    at = _on_device(stream, codes, scales, w_codes, w_scales, c)
     pc, ldc = _matrix(c, (n, n_out), c.dtype, "c")
     px, pxs = _code_rows(codes, scales, n, n_in, n, "codes")
     pw, pws = _code_rows(w_codes, w_scales, n_out, n_in, -(-n_out // CODE_BLOCK), "w_codes")
-    _check(lib().varco_scaled_transform(dt, n, n_in, n_out, px, pxs, pw, pws, pc, ldc, int(accumulate), act, _stream(stream)))
+    _check(lib().varco_scaled_transform(dt, n, n_in, n_out, px, pxs, pw, pws, pc, ldc, int(accumulate), act, at))
 
 
 def scaled_weight_workspace(n_rows, n_in, n_out) -> int:
@@ -366,27 +378,26 @@ def scaled_weight_workspace(n_rows, n_in, n_out) -> int:
 
 def scaled_bwd_weight(y_codes, y_scales, d_codes, d_scales, dh, accumulate=False, workspace=None, stream=None):
     """dh (+)= Y^T D, dh [n_in, n_out] fp32, from rows of codes of the inputs and of the errors."""
-    import torch
     n, (n_in, n_out) = y_codes.shape[0], _rows(dh, "dh")
-    _on_device(stream, y_codes, y_scales, d_codes, d_scales, dh, workspace)
-    ph, ldh = _matrix(dh, (n_in, n_out), torch.float32, "dh")
+    at = _on_device(stream, y_codes, y_scales, d_codes, d_scales, dh, workspace)
+    ph, ldh = _matrix(dh, (n_in, n_out), _torch.float32, "dh")
     py, pys = _code_rows(y_codes, y_scales, n, n_in, n, "y_codes")
     pd, pds = _code_rows(d_codes, d_scales, n, n_out, n, "d_codes")
     pw, size, held = _scratch(scaled_weight_workspace(n, n_in, n_out) if workspace is None else 0, workspace, dh.device, stream)
-    _check(lib().varco_scaled_bwd_weight(n, n_in, n_out, py, pys, pd, pds, ph, ldh, int(accumulate), pw, size, _stream(stream)))
+    _check(lib().varco_scaled_bwd_weight(n, n_in, n_out, py, pys, pd, pds, ph, ldh, int(accumulate), pw, size, at))
 
 
 def rms_norm_fwd(x, gain, eps, residual=None, total=None, y=None, codes=None, scales=None, inv_rms=None, stream=None):
     """u = x + residual, y = u gain / sqrt(mean u^2 + eps); writes what is given of total (u), y, codes with scales, inv_rms."""
     dt, (n, w) = _dtype(x), _rows(x, "x")
-    _on_device(stream, x, gain, residual, total, y, codes, scales, inv_rms)
+    at = _on_device(stream, x, gain, residual, total, y, codes, scales, inv_rms)
     px, ldx = _matrix(x, (n, w), x.dtype, "x")
     pr, ldr = _matrix(residual, (n, w), x.dtype, "residual")
     pt, ldt = _matrix(total, (n, w), x.dtype, "total")
     py, ldy = _matrix(y, (n, w), x.dtype, "y")
     pc, ps = _code_rows(codes, scales, n, w, n, "codes")
     _check(lib().varco_rms_norm_fwd(dt, n, w, px, ldx, pr, ldr, _vector(gain, w, "gain"), eps, pt, ldt, py, ldy, pc, ps,
-                                    _vector(inv_rms, n, "inv_rms"), _stream(stream)))
+                                    _vector(inv_rms, n, "inv_rms"), at))
 
 
 def rms_norm_workspace(dtype, n_rows, width) -> int:
@@ -398,14 +409,14 @@ def rms_norm_workspace(dtype, n_rows, width) -> int:
 def rms_norm_bwd(dy, u, gain, inv_rms, dx=None, dgain=None, dtotal=None, accumulate=False, workspace=None, stream=None):
     """dx = gradient of u through the norm (+ dtotal); dgain (+)= the gain's gradient."""
     dt, (n, w) = _dtype(dy), _rows(dy, "dy")
-    _on_device(stream, dy, u, gain, inv_rms, dx, dgain, dtotal, workspace)
+    at = _on_device(stream, dy, u, gain, inv_rms, dx, dgain, dtotal, workspace)
     pd, ldd = _matrix(dy, (n, w), dy.dtype, "dy")
     pu, ldu = _matrix(u, (n, w), dy.dtype, "u")
     pt, ldt = _matrix(dtotal, (n, w), dy.dtype, "dtotal")
     px, ldx = _matrix(dx, (n, w), dy.dtype, "dx")
     pw, size, held = _scratch(rms_norm_workspace(dt, n, w) if workspace is None and dgain is not None else 0, workspace, dy.device, stream)
     _check(lib().varco_rms_norm_bwd(dt, n, w, pd, ldd, pu, ldu, _vector(gain, w, "gain"), _vector(inv_rms, n, "inv_rms"), pt, ldt, px, ldx,
-                                    _vector(dgain, w, "dgain"), int(accumulate), pw, size, _stream(stream)))
+                                    _vector(dgain, w, "dgain"), int(accumulate), pw, size, at))
 
 
 class TensorList:
@@ -450,8 +461,7 @@ def _same_sizes(a, b):
 
 
 def _limit_out(out):
-    import torch
-    if out is None or out.dtype != torch.float32 or out.numel() != 2 or not out.is_contiguous():
+    if out is None or out.dtype != _torch.float32 or out.numel() != 2 or not out.is_contiguous():
         _refuse(ERR_SHAPE, "out: 2 consecutive float32 values are needed")
     return out.data_ptr()
 
@@ -459,9 +469,9 @@ def _limit_out(out):
 def gradient_norm(grads, max_norm, out, workspace=None, stream=None):
     """out[0] = norm of all tensors of `grads` together, out[1] = min(1, max_norm / norm)."""
     g = _listed(grads)
-    _on_device(stream, out, workspace, *g.tensors[:1])
+    at = _on_device(stream, out, workspace, *g.tensors[:1])
     pw, size, held = _scratch(g.need, workspace, out.device, stream)
-    _check(lib().varco_gradient_norm(g.dtype, len(g), g.pointers, g.sizes, max_norm, _limit_out(out), pw, size, _stream(stream)))
+    _check(lib().varco_gradient_norm(g.dtype, len(g), g.pointers, g.sizes, max_norm, _limit_out(out), pw, size, at))
 
 
 def clip_gradients(grads, max_norm, out, into=None, workspace=None, stream=None):
@@ -469,9 +479,9 @@ def clip_gradients(grads, max_norm, out, into=None, workspace=None, stream=None)
     g = _listed(grads)
     to = g if into is None else _listed(into)
     _same_sizes(g, to)
-    _on_device(stream, out, workspace, *g.tensors[:1], *to.tensors[:1])
+    at = _on_device(stream, out, workspace, *g.tensors[:1], *to.tensors[:1])
     pw, size, held = _scratch(g.need, workspace, out.device, stream)
-    _check(lib().varco_clip_gradients(g.dtype, len(g), g.pointers, to.pointers, g.sizes, max_norm, _limit_out(out), pw, size, _stream(stream)))
+    _check(lib().varco_clip_gradients(g.dtype, len(g), g.pointers, to.pointers, g.sizes, max_norm, _limit_out(out), pw, size, at))
 
 
 def sgd_step_clipped(w, dw, lr, max_norm, out, workspace=None, stream=None):
@@ -480,9 +490,9 @@ def sgd_step_clipped(w, dw, lr, max_norm, out, workspace=None, stream=None):
     _same_sizes(g, to)
     if g.dtype != F32:
         _refuse(ERR_UNSUPPORTED, "weights and their gradients are float32")
-    _on_device(stream, out, workspace, *g.tensors[:1], *to.tensors[:1])
+    at = _on_device(stream, out, workspace, *g.tensors[:1], *to.tensors[:1])
     pw, size, held = _scratch(g.need, workspace, out.device, stream)
-    _check(lib().varco_sgd_step_clipped(len(g), to.pointers, g.pointers, g.sizes, lr, max_norm, _limit_out(out), pw, size, _stream(stream)))
+    _check(lib().varco_sgd_step_clipped(len(g), to.pointers, g.pointers, g.sizes, lr, max_norm, _limit_out(out), pw, size, at))
 
 
 # ---------------------------------------------------------------------------------------------------------

@@ -172,16 +172,16 @@ def test_workspace_queries_refuse_no_output(name, args):
 
 def test_streams_of_another_device_are_refused(monkeypatch):
     class Stream:
-        cuda_stream, device_index = 0, 1
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+        cuda_stream, device_index = 64, 1
+    vb._load_torch()
+    monkeypatch.setattr(vb, "_device", lambda: 0)
     with pytest.raises(vb.VarcoError) as e:
         vb._on_device(Stream())
     assert e.value.code == vb.ERR_INVALID_ARG
     Stream.device_index = 0
-    vb._on_device(Stream())
-    vb._on_device(None, None)
+    assert vb._on_device(Stream(), None) == Stream.cuda_stream
     with pytest.raises(vb.VarcoError):
-        vb._on_device(None, torch.zeros(1))
+        vb._on_device(Stream(), torch.zeros(1))
 
 
 @pytest.mark.parametrize("workspace", [torch.zeros(1, dtype=torch.uint8).expand(4096), torch.zeros(8192, dtype=torch.uint8)[::2]])
