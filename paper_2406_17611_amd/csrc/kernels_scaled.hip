@@ -488,6 +488,81 @@ __global__ __launch_bounds__(kThreads, 1) void scaled_big_kernel(ScaledArgs a, i
     }
 }
 
+// Long reductions over few rows, where the tiles above would leave most compute units idle and each of theirs would wait for one block of the reduction
+// after the other: 32 rows x 32 outputs per workgroup, its eight wavefronts take every eighth block of 128, fragments straight from memory, and
+// join their sums in LDS in one order. Up to 640 workgroups: every one reads its rows and weights anew. (us, so / by the tiles: 1 row 2048 -> 2048 7.9 / 13.5, fp32
+// 7.9 / 19.6, 1 row 16,384 -> 4096 26 / 92; 320 workgroups, 300 rows 8192 -> 1000 38 / 54; 640, 300 rows 2048 -> 2048 15.4 / 16.5; 1,000, 4,000 rows
+// 2048 -> 256 18.8 / 16.2; 1,024, 500 rows 2048 -> 2048 19.3 / 16.7.)
+template <typename T>
+__global__ __launch_bounds__(512) void scaled_few_kernel(ScaledArgs a) {
+    constexpr int WAVES = 8, M = 2, N = 2, F = RowPiece<T>::P / 4;
+    __shared__ floatx4 sums[WAVES][M][N][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, l = lane & 15;
+    const int64_t m0 = int64_t(blockIdx.y) * (16 * M), ld = code_ld(a.n_in), lds = scale_ld(a.n_in);
+    const int32_t n0 = int32_t(blockIdx.x) * (16 * N), steps = (a.n_in + BK - 1) / BK;
+    const uint8_t *x[M], *w[N], *sx[M];
+#pragma unroll
+    for (int j = 0; j < M; ++j) {
+        const int64_t row = min(m0 + 16 * j + l, a.n_rows - 1);
+        x[j] = a.x + row * ld, sx[j] = a.x_scales + row * lds;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = a.w + int64_t(min(n0 + output_of<T>(i, l), a.n_out - 1)) * ld;
+    const uint8_t* const sw = a.w_scales + int64_t(n0 / kCodeBlock) * lds;
+    floatx4 acc[M][N];
+#pragma unroll
+    for (int j = 0; j < M; ++j)
+#pragma unroll
+        for (int i = 0; i < N; ++i) acc[j][i] = floatx4(0.f);
+    auto fragment = [&](const uint8_t* row, int32_t s) {
+        const int64_t k = int64_t(s) * BK + 16 * g;
+        uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo;
+        if (k < ld) lo = *reinterpret_cast<const uint4*>(row + k);
+        if (k + 64 < ld) hi = *reinterpret_cast<const uint4*>(row + k + 64);
+        return joined(lo, hi);
+    };
+#pragma unroll 2
+    for (int32_t s = wave; s < steps; s += WAVES) {
+        intx8 fx[M], fw[N];
+        int scale_x[M];
+#pragma unroll
+        for (int i = 0; i < N; ++i) fw[i] = fragment(w[i], s);
+#pragma unroll
+        for (int j = 0; j < M; ++j) fx[j] = fragment(x[j], s), scale_x[j] = sx[j][s];
+        const int scale_w = sw[s];
+#pragma unroll
+        for (int j = 0; j < M; ++j)
+            if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) acc[j][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[i], fx[j], acc[j][i], 0, 0, 0, scale_w, 0, scale_x[j]);
+            } else {
+                const Bf16Fragment bx(fx[j], scale_x[j]);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const Bf16Fragment bw(fw[i], scale_w);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw.f[q], bx.f[q], acc[j][i], 0, 0, 0);
+                }
+            }
+    }
+#pragma unroll
+    for (int j = 0; j < M; ++j)
+#pragma unroll
+        for (int i = 0; i < N; ++i) sums[wave][j][i][lane] = acc[j][i];
+    __syncthreads();
+    if (wave >= M * N / F) return;
+    const int j = wave / (N / F), i = wave % (N / F) * F;
+    floatx4 sum[F];
+#pragma unroll
+    for (int f = 0; f < F; ++f) {
+        sum[f] = sums[0][j][i + f][lane];
+#pragma unroll
+        for (int v = 1; v < WAVES; ++v) sum[f] += sums[v][j][i + f][lane];
+    }
+    const int64_t row = m0 + 16 * j + l;
+    if (row < a.n_rows) store_outputs(static_cast<T*>(a.c) + row * a.ldc, n0 + 16 * i, g, a, sum);
+}
+
 // Short reductions (512 at most): bound by reading X and writing c. A wavefront keeps the weights of 16 NI outputs in registers
 // and the workgroup walks over rows, 16 R WR at a time, which are copied to LDS D - 1 steps ahead. WN wavefronts take the same rows, their
 // other outputs. (NI: 4; 2 where fp32 results take more than 256 columns, whose weights are kept as bf16, twice the registers.)
@@ -645,7 +720,10 @@ hipError_t varco_launch_scaled_transform(int dtype, const ScaledArgs& a, hipStre
             };
             using std::integral_constant;
             const int64_t big_n = (a.n_out + kBigTile - 1) / kBigTile, big = (a.n_rows + kBigTile - 1) / kBigTile * big_n;
-            if (a.n_out <= 64)
+            const int64_t few_n = (a.n_out + 31) / 32, few_m = (a.n_rows + 31) / 32;
+            if (few_n * few_m <= 640)
+                hipLaunchKernelGGL(scaled_few_kernel<T>, dim3(unsigned(few_n), unsigned(few_m)), dim3(512), 0, stream, a);
+            else if (a.n_out <= 64)
                 tile(integral_constant<int, 4>{}, integral_constant<int, 1>{}, integral_constant<int, 2>{});
             else if (sizeof(T) == 2 && big >= 256 && a.n_rows >= kBigTile && a.n_out >= kBigTile && a.n_in % (2 * BK) == 0 && !a.accumulate)
                 hipLaunchKernelGGL(scaled_big_kernel, dim3(256), dim3(kThreads), 0, stream, a, int32_t(big_n), int32_t(big), whole_lines && a.n_out % 64 == 0);

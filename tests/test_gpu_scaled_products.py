@@ -249,3 +249,25 @@ def test_rows_of_results_at_any_place(dtype, n, n_in, n_out, gap, lead):
     vb.scaled_transform(x8, s8, *turned, n_in, whole[:, :n_out])
     assert bool(((whole[:, :n_out].double() - torch.from_numpy(want).cuda()[at]).abs() <= bound[at]).all())
     assert bool(torch.isnan(whole[:, n_out:]).all()) and bool(torch.isnan(flat[:lead]).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("accumulate,act", [(False, vb.ACT_RELU), (True, vb.ACT_IDENTITY)])
+@pytest.mark.parametrize("n,n_in,n_out", [(1, 16384, 47), (1, 2048, 2048), (31, 700, 130), (300, 1029, 33), (70, 2048, 512),      # a few workgroups
+                                          (5003, 640, 200), (5120, 768, 256), (30011, 1300, 50)])                                 # and tiles beyond them
+def test_long_reductions_over_few_and_more_rows(dtype, n, n_in, n_out, accumulate, act):
+    codes, exps = _coded(min(n, 211), n_in, n)
+    w, turned, _ = _weights(n_in, n_out, n_out)
+    x = oc.values(codes, exps)
+    at = torch.arange(n, device="cuda") % len(codes)
+    x8, s8 = (t[at].contiguous() for t in upload_codes(codes, exps, n_in))
+    start = torch.randn(len(codes), n_out, generator=torch.Generator().manual_seed(4)).to(dtype)
+    c, flat = strided(start.cuda()[at], 5, 1)
+    want, size = x @ w + (f64(start) if accumulate else 0.0), np.abs(x) @ np.abs(w) + np.abs(f64(start))
+    if act == vb.ACT_RELU:
+        want = np.maximum(want, 0.0)
+    vb.scaled_transform(x8, s8, *turned, n_in, c, accumulate=accumulate, act=act)
+    sums = (n_in + 1) * 2.0 ** -24 * size + _dropped_few(dtype, x, w)
+    bound = torch.from_numpy(sums + STEP[dtype] * (np.abs(want) + sums) + 1e-38).cuda()
+    assert bool(((c.double() - torch.from_numpy(want).cuda()[at]).abs() <= bound[at]).all())
+    assert bool(torch.isnan(flat[1:].view(n, n_out + 5)[:, n_out:]).all()) and bool(torch.isnan(flat[0]))
