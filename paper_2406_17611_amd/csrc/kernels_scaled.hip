@@ -186,8 +186,9 @@ template <typename T>
 __device__ __forceinline__ int place_w(int row) { return sizeof(T) == 2 ? (row & 3) | ((row >> 1) & 4) : row & 7; }
 
 // Long reductions over fewer tiles, and what scaled_big_kernel does not take: tiles of 16 MI WM rows x 64 WN outputs, a block of 128 of the
-// reduction at a time through LDS, copied there while the block before is multiplied (two buffers). 128 x 256 where that makes 256
-// tiles, else 128 x 128, two workgroups per compute unit; 128 x 64 for at most 64 outputs.
+// reduction at a time through LDS, copied there while the block before is multiplied (two buffers). 128 x 128, two workgroups per compute unit;
+// fp32 128 x 256 where that makes 256 tiles and no more padding; 128 x 64 for at most 64 outputs. (us, 128 x 256 / 128 x 128: bf16 300,000 rows 640 -> 128 110 / 65,
+// 100,000 rows 1000 -> 1000 231 / 213, 94,484 rows 1024 -> 600 106 / 110; fp32 94,484 rows 1024 -> 512 116 / 125, 100,000 rows 1025 -> 512 157 / 150.)
 template <typename T, int WM, int WN, int MI>
 __global__ __launch_bounds__(64 * WM * WN, 2) void scaled_tile_kernel(ScaledArgs a, int32_t tiles_n, int32_t tiles, bool whole_lines) {
     constexpr int WAVES = WM * WN, BM = 16 * MI * WM, BN = 64 * WN, NX = BM / 8 / WAVES, NW = BN / 8 / WAVES;
@@ -727,8 +728,8 @@ hipError_t varco_launch_scaled_transform(int dtype, const ScaledArgs& a, hipStre
                 tile(integral_constant<int, 4>{}, integral_constant<int, 1>{}, integral_constant<int, 2>{});
             else if (sizeof(T) == 2 && big >= 256 && a.n_rows >= kBigTile && a.n_out >= kBigTile && a.n_in % (2 * BK) == 0 && !a.accumulate)
                 hipLaunchKernelGGL(scaled_big_kernel, dim3(256), dim3(kThreads), 0, stream, a, int32_t(big_n), int32_t(big), whole_lines && a.n_out % 64 == 0);
-            else if (2 * big >= 256)
-                tile(integral_constant<int, 2>{}, integral_constant<int, 4>{}, integral_constant<int, 4>{});
+            else if (sizeof(T) == 4 && 2 * big >= 256 && (a.n_out + 127) / 128 % 2 == 0)
+                tile(integral_constant<int, 2>{}, integral_constant<int, sizeof(T) == 4 ? 4 : 2>{}, integral_constant<int, 4>{});
             else
                 tile(integral_constant<int, 2>{}, integral_constant<int, 2>{}, integral_constant<int, 4>{});
             return;
