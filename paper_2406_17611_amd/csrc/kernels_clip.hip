@@ -1,10 +1,10 @@
 // The norm of all gradients together, and gradients limited to it: out = f g or w -= lr f g with f = min(1, limit / norm).
 // Squares are summed in fp64 (a square of an fp32 number is exact there and neither overflows nor vanishes, and 300 million of them keep
 // 1e-13): the multiprocessors have that to spare, the kernels are bound by reading the gradients.
-// Two launches per 128 tensors: sums of squares per workgroup, then each workgroup of the second launch adds those few
-// sums itself, in one order, instead of a third launch that does it once (six matrices of a small network: 10.1 us, 11.5 with it). The sums of
-// several launches are added once (5,000 tensors of 60 million elements, 40,000 sums, clipped copies 849 us, 1,008 without).
-// 403 tensors of 300 million fp32 elements: norm 194 us (6.2 TB/s), clipped copies 664 us, step 874 us (5.4 TB/s; with loads and stores that the
+// A launch per 284 tensors for the sums of squares per workgroup, then one per 180 that scales: with one of each, its workgroups add those few sums
+// themselves, in one order, instead of a launch in between that does it once (six matrices of a small network: 10.1 us, 11.5 with it). The sums of
+// several launches are added once (5,000 tensors of 60 million elements, clipped copies 567 us; every workgroup for itself, 128 tensors a launch: 1,008).
+// 403 tensors of 300 million fp32 elements: norm 186 us (6.5 TB/s), clipped copies 661 us, step 867 us (5.5 TB/s; with loads and stores that the
 // caches keep 219, 744, 978).
 #include <algorithm>
 #include <type_traits>
@@ -15,8 +15,8 @@
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTensors = 128;        // of one launch: their table is a kernel argument (4 KiB at most; 16 tensors, as a network of a few layers has, fill a smaller one)
-constexpr int kFewTensors = 16;
+// Tensors of one launch: their table is a kernel argument (4 KiB at most; 16 tensors, as a network of a few layers has, fill a smaller one).
+constexpr int kRead = 284, kScaled = 180, kFewTensors = 16;
 constexpr int kWorkgroups = 1024;    // that sum the squares of one launch
 constexpr int kOwnSums = 1024;       // partial sums (one launch's) that every workgroup adds itself; more are added once, in a launch of its own
 
@@ -25,15 +25,17 @@ template <int N>
 struct Table {
     static constexpr int kMost = N;
     const void* src[N];
-    int64_t n[N];
     int32_t first[N + 1];
-    int32_t tensors, chunk;          // elements of a chunk: a multiple of 1024
+    int32_t tensors, chunk;          // elements of a chunk: a multiple of 1024, 16,384 at most
+    uint16_t missing[N];             // elements that a tensor's last chunk lacks
+
+    __device__ __forceinline__ int32_t elements(int k, int32_t c) const { return chunk - (c + 1 == first[k + 1] ? missing[k] : 0); }
 };
 template <int N>
 struct OutTable : Table<N> {
     void* dst[N];
 };
-static_assert(sizeof(OutTable<kTensors>) + 64 <= 4096, "a kernel's arguments");
+static_assert(sizeof(Table<kRead>) + 64 <= 4096 && sizeof(OutTable<kScaled>) + 64 <= 4096, "a kernel's arguments");
 
 // The tensor that chunk c belongs to.
 template <typename TABLE>
@@ -72,7 +74,7 @@ __global__ __launch_bounds__(kThreads) void square_sums_kernel(TABLE t, double* 
         const int k = tensor_of(t, c);
         const int64_t at = int64_t(c - t.first[k]) * t.chunk;
         const T* const p = static_cast<const T*>(t.src[k]) + at;
-        const int32_t n = int32_t(min(int64_t(t.chunk), t.n[k] - at));
+        const int32_t n = t.elements(k, c);
         auto add = [&](auto any) {
 #pragma unroll 4
             for (int32_t i = threadIdx.x * P; i < n; i += kThreads * P) {
@@ -120,7 +122,7 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(TABLE t, const double* 
         const T* const p = static_cast<const T*>(t.src[k]) + at;
         T* const q = static_cast<T*>(t.dst[k]) + at;
         if (!STEP && same && p == q) continue;             // in place and within the limit: the elements stay as they are
-        const int32_t n = int32_t(min(int64_t(t.chunk), t.n[k] - at));
+        const int32_t n = t.elements(k, c);
         auto scale = [&](auto any) {
             constexpr bool ANY = decltype(any)::value;
 #pragma unroll 4
@@ -149,11 +151,11 @@ int64_t total_of(int32_t n_tensors, const int64_t* sizes) {
 int32_t chunk_of(int64_t total) { return int32_t(1024 * std::max<int64_t>(1, std::min<int64_t>(16, total / (1024 * 2048)))); }
 int64_t chunks_of(int64_t n, int64_t chunk) { return (n + chunk - 1) / chunk; }
 
-// Calls f(first tensor, tensors, chunks before, chunks) for each launch.
+// Calls f(first tensor, tensors, chunks) for each launch of `most` tensors.
 template <typename F>
-void over_launches(int32_t n_tensors, const int64_t* sizes, int64_t chunk, F f) {
-    for (int32_t i = 0; i < n_tensors; i += kTensors) {
-        const int32_t n = std::min(kTensors, n_tensors - i);
+void over_launches(int32_t most, int32_t n_tensors, const int64_t* sizes, int64_t chunk, F f) {
+    for (int32_t i = 0; i < n_tensors; i += most) {
+        const int32_t n = std::min(most, n_tensors - i);
         int64_t chunks = 0;
         for (int32_t k = 0; k < n; ++k) chunks += chunks_of(sizes[i + k], chunk);
         if (chunks) f(i, n, chunks);
@@ -164,19 +166,20 @@ template <typename TABLE>
 void fill(TABLE& t, int32_t i, int32_t n, const void* const* src, const int64_t* sizes, int32_t chunk) {
     int64_t c = 0;
     for (int32_t k = 0; k < n; ++k) {
-        t.src[k] = src[i + k], t.n[k] = sizes[i + k], t.first[k] = int32_t(c);
-        c += chunks_of(sizes[i + k], chunk);
+        const int64_t chunks = chunks_of(sizes[i + k], chunk);
+        t.src[k] = src[i + k], t.first[k] = int32_t(c), t.missing[k] = uint16_t(chunks * chunk - sizes[i + k]);
+        c += chunks;
     }
     t.first[n] = int32_t(c);
     t.tensors = n, t.chunk = chunk;
 }
 
-template <typename F>
+template <int MOST, typename F>
 void with_table(int32_t tensors, F f) {
     if (tensors <= kFewTensors)
         f(std::integral_constant<int, kFewTensors>{});
     else
-        f(std::integral_constant<int, kTensors>{});
+        f(std::integral_constant<int, MOST>{});
 }
 
 template <typename T, bool STEP>
@@ -185,8 +188,8 @@ hipError_t launch_scale(int32_t n_tensors, const void* const* src, void* const* 
     const int32_t chunk = chunk_of(total_of(n_tensors, sizes));
     hipError_t err = hipSuccess;
     if (n_partial > kOwnSums) err = varco_launch_norm_out(partial, n_partial, max_norm, out, stream), n_partial = 0;
-    over_launches(n_tensors, sizes, chunk, [&](int32_t i, int32_t n, int64_t chunks) {
-        with_table(n, [&](auto most) {
+    over_launches(kScaled, n_tensors, sizes, chunk, [&](int32_t i, int32_t n, int64_t chunks) {
+        with_table<kScaled>(n, [&](auto most) {
             using TABLE = OutTable<decltype(most)::value>;
             TABLE t;
             fill(t, i, n, src, sizes, chunk);
@@ -205,7 +208,7 @@ hipError_t launch_scale(int32_t n_tensors, const void* const* src, void* const* 
 int32_t varco_clip_partials(int32_t n_tensors, const int64_t* sizes) {
     const int32_t chunk = chunk_of(total_of(n_tensors, sizes));
     int64_t n = 0;
-    over_launches(n_tensors, sizes, chunk, [&](int32_t, int32_t, int64_t chunks) { n += workgroups(chunks); });
+    over_launches(kRead, n_tensors, sizes, chunk, [&](int32_t, int32_t, int64_t chunks) { n += workgroups(chunks); });
     return int32_t(n);
 }
 
@@ -213,9 +216,9 @@ hipError_t varco_launch_square_sums(int dtype, int32_t n_tensors, const void* co
                                     hipStream_t stream) {
     const int32_t chunk = chunk_of(total_of(n_tensors, sizes));
     hipError_t err = hipSuccess;
-    over_launches(n_tensors, sizes, chunk, [&](int32_t i, int32_t n, int64_t chunks) {
+    over_launches(kRead, n_tensors, sizes, chunk, [&](int32_t i, int32_t n, int64_t chunks) {
         const int64_t blocks = workgroups(chunks);
-        with_table(n, [&](auto most) {
+        with_table<kRead>(n, [&](auto most) {
             using TABLE = Table<decltype(most)::value>;
             TABLE t;
             fill(t, i, n, grads, sizes, chunk);

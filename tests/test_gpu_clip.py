@@ -121,6 +121,29 @@ def test_more_tensors_than_a_launch_takes(sizes):
         assert_within(f64(a), f * f64(s), 3 * F * np.abs(f * f64(s)) + 1e-38, "in place")
 
 
+@pytest.mark.parametrize("count", [16, 17, 180, 181, 284, 285, 361, 569])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_as_many_tensors_as_launches_take(count, dtype):
+    """Sizes that end a chunk, exceed it by one or leave one out, and none at all at either end."""
+    sizes = [0] + [(1024, 1023, 1025, 0, 3, 2048)[i % 6] for i in range(count - 2)] + [0]
+    grads, flat = _tensors(sizes, dtype, 7)
+    into, other = _tensors(sizes, dtype, 8)
+    between = other.clone()
+    norm, f = oc.limit([f64(g) for g in grads], 3.0)
+    out = torch.empty(2, device="cuda")
+    vb.clip_gradients(grads, 3.0, out, into=into)
+    assert_within(f64(out), [norm, f], 2 * F * np.array([norm, f]), "norm and factor")
+    for a, g in zip(into, grads):
+        at = slice(a.storage_offset(), a.storage_offset() + a.numel())
+        between[at].copy_(a)
+    assert torch.equal(other, between)
+    want = f * f64(flat)
+    keep = np.zeros(flat.numel(), dtype=bool)
+    for g in grads:
+        keep[g.storage_offset():g.storage_offset() + g.numel()] = True
+    assert_within(f64(other)[keep], want[keep], (2 * F + STEP[dtype]) * np.abs(want[keep]) + 1e-38, "into")
+
+
 def test_limits_of_nothing_and_everything():
     g = [torch.randn(50, device="cuda")]
     keep = g[0].clone()
