@@ -212,10 +212,13 @@ void launch(Tile<WI, WJ, MI, NJ, BK>, const ScaledWeightArgs& a, int32_t split, 
                        tiles_j, tiles);
 }
 
-// Tiles of 256 x 256 where the weights have more than 128 rows and columns and a workgroup per compute unit gets 512 rows or more; else
-// 128 x 128, and 64 on a side of at most 64. (512 x 512 weights, tiles of 256 / of 128: 20,000 rows, 313 each, 36.9 / 30.8 us; 169,343 rows, 2,646 each,
-// 114 / 168; 256 x 256 over 169,343 rows, 661 each, 49.5 / 58; tiles of 128 x 256, half the sums, there 47.9, over 410,003 rows 93, 87 so.)
+// Tiles of 256 x 256 where the weights have more than 128 rows and columns and a workgroup per compute unit gets 512 rows or more, 128 x 256 or 256 x 128
+// where one side has 65 to 128; else 128 x 128, and 64 on a side of at most 64. (512 x 512 weights, tiles of 256 / of 128: 20,000 rows, 313 each, 36.9 /
+// 30.8 us; 169,343 rows, 2,646 each, 114 / 168; 256 x 256 over 169,343 rows, 661 each, 49.5 / 58; tiles of 128 x 256, half the sums, there 47.9, over 410,003
+// rows 93, 87 so. 128 x 512 over 500,000 rows, 128 x 256 / 128 x 128: 106 / 130; 96 x 914 over 125,702 56 / 71; 120 x 300 over 1,000,000 183 / 179.)
 using Big = Tile<2, 4, 8, 4, 64>;
+using Wide = Tile<2, 4, 4, 4, 64>;
+using Tall = Tile<4, 2, 4, 4, 64>;
 using Middle = Tile<2, 2, 4, 4, 32>;
 using Narrow = Tile<2, 2, 4, 2, 64>;
 using Flat = Tile<2, 2, 2, 4, 64>;
@@ -224,9 +227,13 @@ using Small = Tile<2, 2, 2, 2, 64>;
 // Calls f(tile, workgroups that are wanted).
 template <typename F>
 void with_tile(int64_t n_rows, int32_t n_in, int32_t n_out, F f) {
-    const int64_t big = int64_t((n_in + 255) / 256) * ((n_out + 255) / 256);
-    if (n_in > 128 && n_out > 128 && n_rows * big >= int64_t(256) * 512)
+    const bool many = n_rows * int64_t((n_in + 255) / 256) * ((n_out + 255) / 256) >= int64_t(256) * 512;
+    if (many && n_in > 128 && n_out > 128)
         f(Big{}, 256);
+    else if (many && n_in > 64 && n_out > 128)
+        f(Wide{}, 256);
+    else if (many && n_in > 128 && n_out > 64)
+        f(Tall{}, 256);
     else if (n_in > 64 && n_out > 64)
         f(Middle{}, 512);
     else if (n_in > 64)

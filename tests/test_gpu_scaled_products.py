@@ -191,7 +191,7 @@ def test_many_rows(dtype, n, n_in, n_out, act, accumulate):
     assert bool(((c.double() - want[at]).abs() <= bound[at]).all())
 
 
-@pytest.mark.parametrize("n,n_in,n_out", [(70001, 256, 256), (33000, 300, 520), (200003, 47, 100), (20011, 513, 600)])
+@pytest.mark.parametrize("n,n_in,n_out", [(70001, 256, 256), (33000, 300, 520), (200003, 47, 100), (20011, 513, 600), (140003, 100, 200), (70003, 520, 97), (131073, 128, 256), (131101, 256, 65)])
 def test_weight_gradient_over_many_rows(n, n_in, n_out):
     """Rows that repeat: the sum over them is the one over a period, weighted."""
     period = 257
