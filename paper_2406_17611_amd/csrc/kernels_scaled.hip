@@ -490,13 +490,13 @@ __global__ __launch_bounds__(kThreads, 1) void scaled_big_kernel(ScaledArgs a, i
 }
 
 // Long reductions over few rows, where the tiles above would leave most compute units idle and each of theirs would wait for one block of the reduction
-// after the other: 32 rows x 32 outputs per workgroup, its eight wavefronts take every eighth block of 128, fragments straight from memory, and
-// join their sums in LDS in one order. Up to 640 workgroups: every one reads its rows and weights anew. (us, so / by the tiles: 1 row 2048 -> 2048 7.9 / 13.5, fp32
-// 7.9 / 19.6, 1 row 16,384 -> 4096 26 / 92; 320 workgroups, 300 rows 8192 -> 1000 38 / 54; 640, 300 rows 2048 -> 2048 15.4 / 16.5; 1,000, 4,000 rows
-// 2048 -> 256 18.8 / 16.2; 1,024, 500 rows 2048 -> 2048 19.3 / 16.7.)
-template <typename T>
+// after the other: 16 M rows x 16 N outputs per workgroup, its eight wavefronts take every eighth block of 128, fragments straight from memory, and
+// join their sums in LDS in one order. Every workgroup reads its rows and weights anew: tiles of 32 x 32 up to 512 workgroups, of 64 x 64 up to 256. (us, 32 /
+// 64 / the tiles above: 1 row 2048 -> 2048 7.9 / 11.6 / 13.5, fp32 7.9 / 12.3 / 19.6; 1 row 16,384 -> 4096 26 / - / 92; 200 rows 2048 -> 2048 11.1 / 11.8 /
+// 14; 300 14.8 / 11.7 / 16.5; 500 19.3 / 12.0 / 16.7; 1,000, 512 workgroups of 64 x 64, 36 / 22.6 / 17.5; 1,000 rows 8192 -> 1000 - / 39 / 54.)
+template <typename T, int M, int N>
 __global__ __launch_bounds__(512) void scaled_few_kernel(ScaledArgs a) {
-    constexpr int WAVES = 8, M = 2, N = 2, F = RowPiece<T>::P / 4;
+    constexpr int WAVES = 8, F = RowPiece<T>::P / 4;
     __shared__ floatx4 sums[WAVES][M][N][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, l = lane & 15;
     const int64_t m0 = int64_t(blockIdx.y) * (16 * M), ld = code_ld(a.n_in), lds = scale_ld(a.n_in);
@@ -551,17 +551,18 @@ __global__ __launch_bounds__(512) void scaled_few_kernel(ScaledArgs a) {
 #pragma unroll
         for (int i = 0; i < N; ++i) sums[wave][j][i][lane] = acc[j][i];
     __syncthreads();
-    if (wave >= M * N / F) return;
-    const int j = wave / (N / F), i = wave % (N / F) * F;
-    floatx4 sum[F];
+    for (int piece = wave; piece < M * N / F; piece += WAVES) {
+        const int j = piece / (N / F), i = piece % (N / F) * F;
+        floatx4 sum[F];
 #pragma unroll
-    for (int f = 0; f < F; ++f) {
-        sum[f] = sums[0][j][i + f][lane];
+        for (int f = 0; f < F; ++f) {
+            sum[f] = sums[0][j][i + f][lane];
 #pragma unroll
-        for (int v = 1; v < WAVES; ++v) sum[f] += sums[v][j][i + f][lane];
+            for (int v = 1; v < WAVES; ++v) sum[f] += sums[v][j][i + f][lane];
+        }
+        const int64_t row = m0 + 16 * j + l;
+        if (row < a.n_rows) store_outputs(static_cast<T*>(a.c) + row * a.ldc, n0 + 16 * i, g, a, sum);
     }
-    const int64_t row = m0 + 16 * j + l;
-    if (row < a.n_rows) store_outputs(static_cast<T*>(a.c) + row * a.ldc, n0 + 16 * i, g, a, sum);
 }
 
 // Short reductions (512 at most): bound by reading X and writing c. A wavefront keeps the weights of 16 NI outputs in registers
@@ -721,10 +722,15 @@ hipError_t varco_launch_scaled_transform(int dtype, const ScaledArgs& a, hipStre
             };
             using std::integral_constant;
             const int64_t big_n = (a.n_out + kBigTile - 1) / kBigTile, big = (a.n_rows + kBigTile - 1) / kBigTile * big_n;
-            const int64_t few_n = (a.n_out + 31) / 32, few_m = (a.n_rows + 31) / 32;
-            if (few_n * few_m <= 640)
-                hipLaunchKernelGGL(scaled_few_kernel<T>, dim3(unsigned(few_n), unsigned(few_m)), dim3(512), 0, stream, a);
-            else if (a.n_out <= 64)
+            auto few = [&](auto m, int64_t most) {
+                constexpr int M = decltype(m)::value;
+                const int64_t few_n = (a.n_out + 16 * M - 1) / (16 * M), few_m = (a.n_rows + 16 * M - 1) / (16 * M);
+                if (few_n * few_m > most) return false;
+                hipLaunchKernelGGL((scaled_few_kernel<T, M, M>), dim3(unsigned(few_n), unsigned(few_m)), dim3(512), 0, stream, a);
+                return true;
+            };
+            if (few(integral_constant<int, 2>{}, 512) || few(integral_constant<int, 4>{}, 256)) return;
+            if (a.n_out <= 64)
                 tile(integral_constant<int, 4>{}, integral_constant<int, 1>{}, integral_constant<int, 2>{});
             else if (sizeof(T) == 2 && big >= 256 && a.n_rows >= kBigTile && a.n_out >= kBigTile && a.n_in % (2 * BK) == 0 && !a.accumulate)
                 hipLaunchKernelGGL(scaled_big_kernel, dim3(256), dim3(kThreads), 0, stream, a, int32_t(big_n), int32_t(big), whole_lines && a.n_out % 64 == 0);

@@ -253,7 +253,7 @@ def test_rows_of_results_at_any_place(dtype, n, n_in, n_out, gap, lead):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("accumulate,act", [(False, vb.ACT_RELU), (True, vb.ACT_IDENTITY)])
-@pytest.mark.parametrize("n,n_in,n_out", [(1, 16384, 47), (1, 2048, 2048), (31, 700, 130), (300, 1029, 33), (70, 2048, 512),      # a few workgroups
+@pytest.mark.parametrize("n,n_in,n_out", [(1, 16384, 47), (1, 2048, 2048), (31, 700, 130), (300, 1029, 33), (70, 2048, 512), (333, 640, 2047), (997, 1100, 835),      # a few workgroups
                                           (5003, 640, 200), (5120, 768, 256), (30011, 1300, 50)])                                 # and tiles beyond them
 def test_long_reductions_over_few_and_more_rows(dtype, n, n_in, n_out, accumulate, act):
     codes, exps = _coded(min(n, 211), n_in, n)
