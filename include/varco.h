@@ -503,15 +503,18 @@ int32_t varco_quantize_rows(int32_t dtype, int64_t n_rows, int32_t width, const 
 int32_t varco_quantize_weights(int32_t n_in, int32_t n_out, const void* h, int64_t ldh, void* turned, void* turned_scales, void* codes,
                                void* scales, varco_stream stream);
 /* c = act((c +) X W), n_rows x n_out of type dtype, X of n_rows x n_in codes, W the n_in x n_out weights given as `turned` above
- * (input gradients: X the codes of the errors, n_in the layer's outputs, W its `codes`). The products of the codes' values are exact. dtype VARCO_F32: sums
- * as accurate as fp32 additions. VARCO_BF16: sums in fp32 of the 8-bit matrix units, which drop of each product what lies 2^-13 below the
+ * (input gradients: X the codes of the errors, n_in the layer's outputs, W its `codes`). dtype VARCO_F32: products of the numbers that codes under
+ * scales 2^-124 .. 2^119 stand for, exact, and sums as accurate as fp32 additions; under smaller scales numbers are taken to the nearest multiple of 2^-133,
+ * and the code 256 under 2^120 (finite numbers from 1.9375 2^127 on become that) stands for 2^128, beyond fp32: what
+ * it takes part in is infinite or NaN. VARCO_BF16: exact products
+ * under all scales, sums in fp32 of the 8-bit matrix units, which drop of each product what lies 2^-13 below the
  * largest of the eight consecutive ones it is added with (an error below 2^-10 of the sum of the products' sizes, typically a tenth of the rounding
  * of c), at twice the rate. One rounding to c. act: VARCO_ACT_*. accumulate != 0 adds to what c holds. c must not overlap an operand. */
 int32_t varco_scaled_transform(int32_t dtype, int64_t n_rows, int32_t n_in, int32_t n_out, const void* codes, const void* scales,
                                const void* w_codes, const void* w_scales, void* c, int64_t ldc, int32_t accumulate, int32_t act,
                                varco_stream stream);
 /* Weight gradient dh = Y^T D (accumulate != 0: added to what dh holds), fp32 n_in x n_out, from rows of codes of the inputs Y (width
- * n_in) and of the errors D (width n_out), summed in fp32 in one order. n_rows = 0 gives 0. */
+ * n_in) and of the errors D (width n_out), summed in fp32 in one order; numbers as for VARCO_F32 above. n_rows = 0 gives 0. */
 int32_t varco_scaled_weight_workspace(int64_t n_rows, int32_t n_in, int32_t n_out, int64_t* bytes);
 int32_t varco_scaled_bwd_weight(int64_t n_rows, int32_t n_in, int32_t n_out, const void* y_codes, const void* y_scales, const void* d_codes,
                                 const void* d_scales, void* dh, int64_t ldh, int32_t accumulate, void* workspace, int64_t workspace_bytes,

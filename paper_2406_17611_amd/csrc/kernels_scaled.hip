@@ -5,8 +5,9 @@
 // ones and drops, of each, what lies below 2^-13 of the group's largest power of two (measured: one product beside two larger
 // ones that cancel; between groups 24 bits and more are kept). Over rows of normal numbers that is 1.5e-4 of the result's norm where
 // the rounding to bf16 is 1.7e-3.
-// fp32 results, which would lose ten bits to that, come from the bf16 units at half the rate: a code times its scale is a bf16
-// number exactly, made of the fragment when it has been read (v_cvt_scalef32_pk_bf16_fp8).
+// fp32 results, which would lose ten bits to that, come from the bf16 units at half the rate: a code times its scale, made of the fragment
+// when it has been read (v_cvt_scalef32_pk_bf16_fp8), is a bf16 number exactly under scales from 2^-124 (its smallest code is 2^-133, the last
+// step of bf16; below, the conversion rounds to that) to 2^119 (256 2^120, the only number beyond, is 2^128 and becomes an infinity, as in fp32).
 // W lies with the reduction consecutive, as X does: a lane's 32 bytes of a fragment are two pieces of 16 bytes, taken as pieces g and
 // g + 4 of the 8 of a block, g = lane / 16, in both operands. (The order inside a block of 128 is free as long as both have the same.)
 // The weights are the first operand: a lane then holds four consecutive outputs of one row.
@@ -31,7 +32,8 @@ __device__ __forceinline__ intx8 joined(const uint4& lo, const uint4& hi) {
     return intx8{int(lo.x), int(lo.y), int(lo.z), int(lo.w), int(hi.x), int(hi.y), int(hi.z), int(hi.w)};
 }
 
-// A fragment's 32 codes as four fragments of the bf16 unit.
+// A fragment's 32 codes as four fragments of the bf16 unit. The scale's exponent + 127 are the upper bits of the fp32 number 2^e; 2^-127 is 0x400000 (the
+// conversion reads the exponent bits, 0 as 2^-127: measured for all 255 scales and all codes).
 struct Bf16Fragment {
     bf16x8 f[4];
     Bf16Fragment() = default;

@@ -1,6 +1,6 @@
 // Weight gradients from codes: dh (+)= sum over rows r of y[r, i] d[r, j]. The scales of both operands change along the reduction (a
-// scale belongs to a row), so they cannot be applied to sums; code times scale is a bf16 number exactly, and the products are formed
-// on the bf16 matrix units from those: nothing is rounded before the fp32 accumulators.
+// scale belongs to a row), so they cannot be applied to sums; code times scale is a bf16 number exactly (scales 2^-124 .. 2^119; what
+// lies beyond is in kernels_scaled.hip), and the products are formed on the bf16 matrix units from those: nothing is rounded before the fp32 accumulators.
 // Codes are turned into bf16 on their way into LDS (v_cvt_scalef32_pk_bf16_fp8, which applies the scale), where they lie as in memory, and
 // are transposed when they are read (ds_read_b64_tr_b16 hands lane i of a group of 16 the i-th column of a 4 x 16 block). Row pitch: 64
 // bytes more than a multiple of 256, so that the four rows of such a block start in four different quarters of the banks.
