@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import weakref
 
 import numpy as np
 
@@ -433,9 +434,10 @@ class TensorList:
                 _refuse(ERR_SHAPE, "a tensor that is not consecutive in memory")
             if t.get_device() != self.tensors[0].get_device() or not t.is_cuda:
                 _refuse(ERR_INVALID_ARG, "tensors on different devices or not on one")
-        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in self.tensors if t.numel())
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), i) for i, t in enumerate(self.tensors) if t.numel())
         if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
             _refuse(ERR_INVALID_ARG, "tensors that overlap")
+        self._spans, self._apart = spans, None
         n = len(self.tensors)
         self.pointers = (C.c_void_p * n)(*[t.data_ptr() for t in self.tensors])
         self.sizes = (C.c_int64 * n)(*[t.numel() for t in self.tensors])
@@ -460,6 +462,26 @@ def _same_sizes(a, b):
         _refuse(ERR_SHAPE, "lists of tensors that do not match")
 
 
+def _check_apart(written, read, in_place):
+    """Refuses to write a list that overlaps the one that is read: workgroups would overwrite what others have yet to read. in_place: a tensor
+    may be the one at its place in the other list. The last verdict stays with the list: a pair that a program steps with is compared once."""
+    known = written._apart
+    if known is not None and known[0]() is read and known[1] == in_place:
+        return
+    if not (in_place and written is read):
+        a, b = written._spans, read._spans
+        i = j = 0
+        while i < len(a) and j < len(b):
+            (start, end, k), (other, other_end, m) = a[i], b[j]
+            if start < other_end and other < end and not (in_place and start == other and k == m):
+                _refuse(ERR_INVALID_ARG, "lists of tensors that overlap")
+            if end <= other_end:
+                i += 1
+            else:
+                j += 1
+    written._apart = weakref.ref(read), in_place
+
+
 def _limit_out(out):
     if out is None or out.dtype != _torch.float32 or out.numel() != 2 or not out.is_contiguous():
         _refuse(ERR_SHAPE, "out: 2 consecutive float32 values are needed")
@@ -475,19 +497,21 @@ def gradient_norm(grads, max_norm, out, workspace=None, stream=None):
 
 
 def clip_gradients(grads, max_norm, out, into=None, workspace=None, stream=None):
-    """gradient_norm, and into[t] = out[1] * grads[t] (into None: in place)."""
+    """gradient_norm, and into[t] = out[1] * grads[t] (into None: in place; else into[t] is grads[t] or overlaps none of them)."""
     g = _listed(grads)
     to = g if into is None else _listed(into)
     _same_sizes(g, to)
+    _check_apart(to, g, True)
     at = _on_device(stream, out, workspace, *g.tensors[:1], *to.tensors[:1])
     pw, size, held = _scratch(g.need, workspace, out.device, stream)
     _check(lib().varco_clip_gradients(g.dtype, len(g), g.pointers, to.pointers, g.sizes, max_norm, _limit_out(out), pw, size, at))
 
 
 def sgd_step_clipped(w, dw, lr, max_norm, out, workspace=None, stream=None):
-    """gradient_norm of dw, and w[t] -= lr * out[1] * dw[t] (fp32)."""
+    """gradient_norm of dw, and w[t] -= lr * out[1] * dw[t] (fp32; w overlaps no gradient)."""
     g, to = _listed(dw), _listed(w)
     _same_sizes(g, to)
+    _check_apart(to, g, False)
     if g.dtype != F32:
         _refuse(ERR_UNSUPPORTED, "weights and their gradients are float32")
     at = _on_device(stream, out, workspace, *g.tensors[:1], *to.tensors[:1])

@@ -1,0 +1,31 @@
+"""Lists of device tensors that are updated together, through the calls that take them."""
+import pytest
+import torch
+
+from paper_2406_17611_amd import binding as vb
+
+pytestmark = pytest.mark.gpu
+
+
+def test_lists_that_overlap_are_refused_and_nothing_is_written():
+    flat = torch.randn(100_000, device="cuda")
+    keep, out = flat.clone(), torch.full((2,), -1.0, device="cuda")
+    grads = [flat[:40_000], flat[50_000:90_000]]
+    shifted, swapped = [flat[4:40_004], flat[50_004:90_004]], grads[::-1]
+    for others in (shifted, swapped, vb.TensorList(shifted)):
+        with pytest.raises(vb.VarcoError):
+            vb.clip_gradients(grads, 0.1, out, into=others)
+        with pytest.raises(vb.VarcoError):
+            vb.sgd_step_clipped(others, grads, 0.1, 0.1, out)
+    with pytest.raises(vb.VarcoError):
+        vb.sgd_step_clipped(grads, grads, 0.1, 0.1, out)
+    assert torch.equal(flat, keep) and (out == -1.0).all()
+
+
+def test_in_place_through_views_of_the_same_memory():
+    flat = torch.randn(1000, device="cuda")
+    want = flat.clone()
+    out, again = torch.empty(2, device="cuda"), torch.empty(2, device="cuda")
+    vb.clip_gradients([want[:300], want[300:]], 0.5, out)
+    vb.clip_gradients([flat[:300], flat[300:]], 0.5, again, into=[flat[:300], flat[300:]])
+    assert torch.equal(flat, want) and torch.equal(out, again)
