@@ -422,10 +422,14 @@ def rms_norm_bwd(dy, u, gain, inv_rms, dx=None, dgain=None, dtotal=None, accumul
 
 class TensorList:
     """Addresses and sizes of tensors that a program updates together, made once: device tensors of one type, each consecutive in
-    memory, none overlapping another. Holds the tensors."""
+    memory, none overlapping another. Holds the tensors; one that has been given other memory since (t.data = ...) is taken where it is
+    when the list is used."""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
+        self._take()
+
+    def _take(self):
         self.dtype = _dtype(self.tensors[0]) if self.tensors else F32
         for t in self.tensors:
             if _dtype(t) != self.dtype:
@@ -434,21 +438,31 @@ class TensorList:
                 _refuse(ERR_SHAPE, "a tensor that is not consecutive in memory")
             if t.get_device() != self.tensors[0].get_device() or not t.is_cuda:
                 _refuse(ERR_INVALID_ARG, "tensors on different devices or not on one")
-        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), i) for i, t in enumerate(self.tensors) if t.numel())
+        at, counts = [t.data_ptr() for t in self.tensors], [t.numel() for t in self.tensors]
+        spans = sorted((p, p + n * t.element_size(), i) for i, (p, n, t) in enumerate(zip(at, counts, self.tensors)) if n)
         if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
             _refuse(ERR_INVALID_ARG, "tensors that overlap")
         self._spans, self._apart = spans, None
-        n = len(self.tensors)
-        self.pointers = (C.c_void_p * n)(*[t.data_ptr() for t in self.tensors])
-        self.sizes = (C.c_int64 * n)(*[t.numel() for t in self.tensors])
+        self.pointers = (C.c_void_p * len(at))(*at)
+        self.sizes = (C.c_int64 * len(at))(*counts)
         self.need = gradient_norm_workspace(self)
+        self._at = list(zip(self.tensors, at, counts))
+
+    def current(self):
+        """The list itself, of the memory that its tensors have now: a step on memory that was given up would write to what has taken its
+        place."""
+        for t, p, n in self._at:
+            if t.data_ptr() != p or t.numel() != n:
+                self._take()
+                break
+        return self
 
     def __len__(self):
         return len(self.tensors)
 
 
 def _listed(tensors):
-    return tensors if isinstance(tensors, TensorList) else TensorList(tensors)
+    return tensors.current() if isinstance(tensors, TensorList) else TensorList(tensors)
 
 
 def gradient_norm_workspace(tensors) -> int:
@@ -466,7 +480,7 @@ def _check_apart(written, read, in_place):
     """Refuses to write a list that overlaps the one that is read: workgroups would overwrite what others have yet to read. in_place: a tensor
     may be the one at its place in the other list. The last verdict stays with the list: a pair that a program steps with is compared once."""
     known = written._apart
-    if known is not None and known[0]() is read and known[1] == in_place:
+    if known is not None and known[0]() is read and known[1] is read._at and known[2] == in_place:
         return
     if not (in_place and written is read):
         a, b = written._spans, read._spans
@@ -479,7 +493,7 @@ def _check_apart(written, read, in_place):
                 i += 1
             else:
                 j += 1
-    written._apart = weakref.ref(read), in_place
+    written._apart = weakref.ref(read), read._at, in_place
 
 
 def _limit_out(out):

@@ -29,3 +29,21 @@ def test_in_place_through_views_of_the_same_memory():
     vb.clip_gradients([want[:300], want[300:]], 0.5, out)
     vb.clip_gradients([flat[:300], flat[300:]], 0.5, again, into=[flat[:300], flat[300:]])
     assert torch.equal(flat, want) and torch.equal(out, again)
+
+
+def test_steps_follow_tensors_to_other_memory():
+    g = torch.Generator().manual_seed(1)
+    weights = [torch.randn(n, generator=g).cuda() for n in (5000, 3, 70_001)]
+    grads = [torch.randn(n, generator=g).cuda() for n in (5000, 3, 70_001)]
+    w, dw, out = vb.TensorList(weights), vb.TensorList(grads), torch.empty(2, device="cuda")
+    vb.sgd_step_clipped(w, dw, 0.1, 1.0, out)
+    old = weights[0].data
+    kept = old.clone()
+    weights[0].data = torch.ones(5000, device="cuda")
+    grads[2].data = torch.randn(70_001, generator=g).cuda()
+    want, norm = [t.clone() for t in weights], torch.empty(2, device="cuda")
+    vb.sgd_step_clipped(list(want), list(grads), 0.1, 1.0, norm)
+    vb.sgd_step_clipped(w, dw, 0.1, 1.0, out)
+    assert torch.equal(out, norm) and torch.equal(old, kept)
+    for a, b in zip(weights, want):
+        assert torch.equal(a, b)

@@ -100,3 +100,41 @@ def test_a_verdict_holds_for_its_pair_only():
         with pytest.raises(vb.VarcoError):
             vb._check_apart(*pair, False)
     vb._check_apart(apart, grads, False)
+
+
+def test_a_tensor_with_other_memory_is_taken_where_it_is_now():
+    """As after t.data = ..., t.set_(...), t.resize_(...): a list never goes on with an address that a tensor no longer has."""
+    tensors = _tensors(*GRADS)
+    made = vb.TensorList(tensors)
+    assert vb._listed(made) is made and list(made.pointers) == [t.address for t in tensors]
+    tensors[2].address = BASE - 4096
+    assert vb._listed(made) is made and list(made.pointers) == [t.address for t in tensors]
+    tensors[1].n = 40
+    assert list(vb._listed(made).sizes) == [100, 40, 100, 100]
+    need = made.need
+    tensors[3].n = 1 << 24
+    assert vb._listed(made).need == vb.gradient_norm_workspace(made) > need
+
+
+def test_other_memory_is_checked_as_a_new_list_is():
+    grads, weights = _tensors(*GRADS), _tensors(2000, 2100, 2200, 2300)
+    g, w = vb.TensorList(grads), vb.TensorList(weights)
+    vb._check_apart(w, g, False)
+    out = Memory(64, 2)
+    for t, address in ((grads[0], BASE + 4 * 2050), (weights[3], BASE + 4 * 150)):
+        keep, t.address = t.address, address
+        for _ in range(2):
+            with pytest.raises(vb.VarcoError) as e:
+                vb.sgd_step_clipped(w, g, 0.1, 1.0, out)
+            assert "overlap" in str(e.value)
+        t.address = keep
+        vb._check_apart(vb._listed(w), vb._listed(g), False)
+    grads[0].address = BASE + 4 * 50                                  # over its neighbour
+    for _ in range(2):
+        with pytest.raises(vb.VarcoError):
+            vb.gradient_norm(g, 1.0, out)
+    grads[0].address = BASE
+    grads[0].n = 99
+    with pytest.raises(vb.VarcoError) as e:
+        vb.sgd_step_clipped(w, g, 0.1, 1.0, out)
+    assert e.value.code == vb.ERR_SHAPE
