@@ -78,7 +78,8 @@ class PartitionedNetwork:
         self._zcap = [0] * self.L
         self._dzcap = [0] * self.L
         self._streams = None
-        self._norm = self._flat_lists = None
+        self._norm = torch.empty(2, dtype=torch.float32, device=self.device)
+        self._flat_lists = None
         self._capture_stream = None        # one for all captures: each stream has a workspace set of its own
         self._prepared = set()
         self._prepare([None])
@@ -323,13 +324,17 @@ class PartitionedNetwork:
                                   self._row_loss[r], self._row_correct[r], self._totals, stream)
         return self._totals
 
+    @property
+    def gradient_norm(self):
+        """Device tensor [norm of all gradients, the factor that limited them] of the last limited step: one tensor, which the next one
+        overwrites (read it after synchronising, or copy it on the step's stream)."""
+        return self._norm
+
     def sgd(self, lr: float, stream=None, max_norm=None):
-        """The gradient step on all weights. max_norm: with the gradients limited to that norm, all of them together; the device tensor
-        [their norm, the factor that limited them] is returned then."""
+        """The gradient step on all weights. max_norm: with the gradients limited to that norm, all of them together; gradient_norm is
+        returned then."""
         w, dw = self._whole(self._h_flat, self.h1, self.h0), self._whole(self._dh_flat, self.dh1, self.dh0)
         if max_norm is not None:
-            if self._norm is None:
-                self._norm = torch.empty(2, dtype=torch.float32, device=self.device)
             if w is not None and dw is not None:
                 if self._flat_lists is None:                 # of the network's own two buffers, which stay
                     self._flat_lists = vb.TensorList([w]), vb.TensorList([dw])

@@ -48,7 +48,7 @@ def run(task, name, ratio_of_step, steps, lr, every, max_norm=None):
             torch.cuda.synchronize()
             curve.append({"step": step + 1, "train_risk": round(risk, 4),
                           "test_accuracy": round(float(t.cpu()[1]) / net.n_test, 4), "bytes_sent": int(sent),
-                          **({} if max_norm is None else {"gradient_norm": round(float(net._norm.cpu()[0]), 5)})})
+                          **({} if max_norm is None else {"gradient_norm": round(float(net.gradient_norm.cpu()[0]), 5)})})
     return {"setting": name, "final_test_accuracy": curve[-1]["test_accuracy"], "bytes_sent": curve[-1]["bytes_sent"],
             "curve": curve}
 
