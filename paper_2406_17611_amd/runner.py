@@ -356,7 +356,10 @@ class PartitionedNetwork:
         self.forward(step, ratio, stream)
         totals = self.loss(True, True, stream)
         self.backward(stream)
-        self.sgd(lr, stream, max_norm)
+        if max_norm is None:
+            self.sgd(lr, stream)                 # (as subclasses with a step of their own define it)
+        else:
+            self.sgd(lr, stream, max_norm)
         return totals
 
     # ------------------------------------------------------------------ HIP graph of one step

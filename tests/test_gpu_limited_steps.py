@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from paper_2406_17611_amd.runner import PartitionedNetwork
 from test_gpu_normalised_layers import _network
 
 pytestmark = pytest.mark.gpu
@@ -23,3 +24,20 @@ def test_norm_and_factor_lie_in_a_buffer_of_the_network():
     returned = net.sgd(0.0, max_norm=0.25)
     assert returned is net.gradient_norm and returned.data_ptr() == at
     assert float(returned[0]) == float(first[0]) and abs(float(returned[1]) - min(1.0, 0.25 / float(first[0]))) < 1e-6
+
+def test_a_subclass_with_a_step_of_its_own_still_trains():
+    class Network(PartitionedNetwork):
+        steps = 0
+
+        def sgd(self, lr, stream=None):
+            Network.steps += 1
+            return super().sgd(lr, stream)
+
+    a, b = _network(), _network()
+    b.__class__ = Network
+    for step in range(2):
+        a.train_step(step, (2, 1), 0.3)
+        b.train_step(step, (2, 1), 0.3)
+    assert Network.steps == 2
+    for x, y in zip(a.h1 + a.h0, b.h1 + b.h0):
+        assert torch.equal(x, y)
