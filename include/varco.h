@@ -478,7 +478,8 @@ int32_t varco_sgd_step(void* w, const void* dw, int64_t n, float lr, varco_strea
  * an element and have any leading dimension >= width. Where a call needs scratch memory the caller
  * passes it: `workspace`, 256-byte aligned, of at least the bytes that the matching *_workspace call names for the same sizes;
  * its contents matter neither before nor after, and it must not be shared by calls (or graphs) that may overlap. 0 bytes: NULL
- * will do. Counts of rows are below 2^31, widths 1 .. VARCO_MAX_CODE_WIDTH.
+ * will do. Counts of rows are below 2^31, widths 1 .. VARCO_MAX_CODE_WIDTH. Matrices and codes that are written must not overlap others, but for the uses in
+ * place that are named (the same rows, at the same leading dimension); the calls refuse it.
  *
  * Codes. A row of `width` numbers is stored as `width` bytes of 4 exponent and 3 fraction bits (e4m3: largest 448, no infinity) and a
  * scale 2^e for each 128 columns, a byte e + 127 (e8m0). a = the largest finite |v| of the block; e is the smallest integer with

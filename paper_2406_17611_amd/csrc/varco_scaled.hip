@@ -38,6 +38,37 @@ int32_t check_matrix(const void* p, int64_t ld, int32_t width, uintptr_t bytes, 
     if (ld < width) return refuse(VARCO_ERR_SHAPE, fn, "leading dimension smaller than the width");
     return VARCO_OK;
 }
+// Rows in memory: n of `bytes` bytes, `step` bytes apart.
+struct Rows {
+    const void* at;
+    int64_t n, bytes, step;
+};
+Rows rows_of(const void* p, int64_t n, int64_t ld, int64_t width, uintptr_t element) {
+    return {p, n, width * int64_t(element), (n > 1 ? ld : width) * int64_t(element)};
+}
+Rows whole(const void* p, int64_t bytes) { return {p, 1, bytes, bytes}; }
+// Whether a byte of a is one of b. Rows as far apart (columns of one wider matrix, say) and a single row are compared row by row, others by where they begin
+// and end.
+bool overlap(const Rows& a, const Rows& b) {
+    if (!a.at || !b.at || a.n < 1 || b.n < 1) return false;
+    if (a.n > 1 && (b.n == 1 || reinterpret_cast<uintptr_t>(b.at) < reinterpret_cast<uintptr_t>(a.at))) return overlap(b, a);
+    const uintptr_t start = reinterpret_cast<uintptr_t>(a.at), other = reinterpret_cast<uintptr_t>(b.at);
+    if (a.n == 1) {                              // the first row of b that ends behind a's start has to begin before a's end
+        const int64_t k = start < other + b.bytes ? 0 : int64_t(start - other - b.bytes) / b.step + 1;
+        return k < b.n && other + k * b.step < start + a.bytes;
+    }
+    if (other >= start + (a.n - 1) * a.step + a.bytes) return false;
+    if (a.step != b.step) return true;
+    const int64_t k = int64_t(other - start) / a.step, into = int64_t(other - start) % a.step;       // b begins in row k of a, or behind it
+    return (k < a.n && into < a.bytes) || (k + 1 < a.n && a.step - into < b.bytes);
+}
+// What is written, against what is read: nothing of one may be the other's, but for all the rows themselves where `in_place`.
+int32_t check_written(const Rows& written, std::initializer_list<Rows> read, bool in_place, const char* fn) {
+    for (const Rows& r : read)
+        if (overlap(written, r) && !(in_place && written.at == r.at && written.step == r.step))
+            return refuse(VARCO_ERR_INVALID_ARG, fn, "an output overlaps what the call reads or another output");
+    return VARCO_OK;
+}
 int32_t check_codes(const void* codes, const void* scales, bool required, const char* fn) {
     if (!codes && !scales && !required) return VARCO_OK;
     if (!codes || !scales) return refuse(VARCO_ERR_INVALID_ARG, fn, "null codes or scales");
@@ -93,6 +124,10 @@ extern "C" int32_t varco_quantize_rows(int32_t dtype, int64_t n_rows, int32_t wi
     VARCO_CHECK(check_matrix(x, ldx, width, element(dtype), true, fn));
     VARCO_CHECK(check_matrix(gate, ldg, width, element(dtype), false, fn));
     VARCO_CHECK(check_codes(codes, scales, true, fn));
+    const Rows code_rows = whole(codes, n_rows * code_ld(width)), scale_rows = whole(scales, n_rows * scale_ld(width));
+    const Rows from = rows_of(x, n_rows, ldx, width, element(dtype)), by = rows_of(gate, n_rows, ldg, width, element(dtype));
+    VARCO_CHECK(check_written(code_rows, {from, by, scale_rows}, false, fn));
+    VARCO_CHECK(check_written(scale_rows, {from, by}, false, fn));
     return result(varco_launch_quantize_rows(dtype, n_rows, width, x, ldx, gate, ldg, static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scales),
                                              static_cast<hipStream_t>(stream)), fn);
 }
@@ -123,6 +158,9 @@ extern "C" int32_t varco_scaled_transform(int32_t dtype, int64_t n_rows, int32_t
     VARCO_CHECK(check_codes(codes, scales, true, fn));
     VARCO_CHECK(check_codes(w_codes, w_scales, true, fn));
     VARCO_CHECK(check_matrix(c, ldc, n_out, element(dtype), true, fn));
+    VARCO_CHECK(check_written(rows_of(c, n_rows, ldc, n_out, element(dtype)),
+                              {whole(codes, n_rows * code_ld(n_in)), whole(scales, n_rows * scale_ld(n_in)), whole(w_codes, n_out * code_ld(n_in)),
+                               whole(w_scales, (n_out + kCodeBlock - 1) / kCodeBlock * scale_ld(n_in))}, false, fn));
     ScaledArgs a;
     a.n_rows = n_rows, a.n_in = n_in, a.n_out = n_out;
     a.x = static_cast<const uint8_t*>(codes), a.x_scales = static_cast<const uint8_t*>(scales);
@@ -154,6 +192,8 @@ extern "C" int32_t varco_scaled_bwd_weight(int64_t n_rows, int32_t n_in, int32_t
         VARCO_CHECK(check_codes(d_codes, d_scales, true, fn));
     }
     VARCO_CHECK(check_workspace(workspace, workspace_bytes, varco_scaled_weight_floats(n_rows, n_in, n_out) * 4, fn));
+    VARCO_CHECK(check_written(rows_of(dh, n_in, ldh, n_out, 4), {whole(y_codes, n_rows * code_ld(n_in)), whole(y_scales, n_rows * scale_ld(n_in)),
+                                                                 whole(d_codes, n_rows * code_ld(n_out)), whole(d_scales, n_rows * scale_ld(n_out))}, false, fn));
     ScaledWeightArgs a;
     a.n_rows = n_rows, a.n_in = n_in, a.n_out = n_out;
     a.y = static_cast<const uint8_t*>(y_codes), a.y_scales = static_cast<const uint8_t*>(y_scales);
@@ -181,6 +221,16 @@ extern "C" int32_t varco_rms_norm_fwd(int32_t dtype, int64_t n_rows, int32_t wid
     VARCO_CHECK(check_codes(codes, scales, false, fn));
     if (!total && !y && !codes && !inv_rms) return refuse(VARCO_ERR_INVALID_ARG, fn, "no output");
     if (total && total == y) return refuse(VARCO_ERR_INVALID_ARG, fn, "total and y are the same memory");
+    const Rows from = rows_of(x, n_rows, ldx, width, e), added = rows_of(residual, n_rows, ldr, width, e);
+    const Rows sum = rows_of(total, n_rows, ldt, width, e), normal = rows_of(y, n_rows, ldy, width, e);
+    VARCO_CHECK(check_written(sum, {from, added}, true, fn));
+    VARCO_CHECK(check_written(normal, {from, added}, true, fn));
+    VARCO_CHECK(check_written(normal, {sum}, false, fn));
+    if (codes) {
+        const Rows code_rows = whole(codes, n_rows * code_ld(width)), scale_rows = whole(scales, n_rows * scale_ld(width));
+        VARCO_CHECK(check_written(code_rows, {from, added, sum, normal, scale_rows}, false, fn));
+        VARCO_CHECK(check_written(scale_rows, {from, added, sum, normal}, false, fn));
+    }
     NormFwdArgs a;
     a.n_rows = n_rows, a.width = width;
     a.x = x, a.ldx = ldx, a.residual = residual, a.ldr = ldr;
@@ -219,6 +269,8 @@ extern "C" int32_t varco_rms_norm_bwd(int32_t dtype, int64_t n_rows, int32_t wid
     VARCO_CHECK(check_matrix(dgain, width, width, 4, false, fn));
     if (!dx && !dgain) return n_rows == 0 ? VARCO_OK : refuse(VARCO_ERR_INVALID_ARG, fn, "no output");
     if (dgain) VARCO_CHECK(check_workspace(workspace, workspace_bytes, norm_bytes(dtype, n_rows, width), fn));
+    VARCO_CHECK(check_written(rows_of(dx, n_rows, lddx, width, e), {rows_of(dy, n_rows, lddy, width, e), rows_of(u, n_rows, ldu, width, e),
+                                                                     rows_of(dtotal, n_rows, lddt, width, e)}, true, fn));
     NormBwdArgs a;
     a.n_rows = n_rows, a.width = width;
     a.dy = dy, a.lddy = lddy, a.u = u, a.ldu = ldu;
