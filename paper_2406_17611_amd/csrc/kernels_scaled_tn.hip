@@ -215,7 +215,9 @@ void launch(Tile<WI, WJ, MI, NJ, BK>, const ScaledWeightArgs& a, int32_t split, 
 // Tiles of 256 x 256 where the weights have more than 128 rows and columns and a workgroup per compute unit gets 512 rows or more, 128 x 256 or 256 x 128
 // where one side has 65 to 128; else 128 x 128, and 64 on a side of at most 64. (512 x 512 weights, tiles of 256 / of 128: 20,000 rows, 313 each, 36.9 /
 // 30.8 us; 169,343 rows, 2,646 each, 114 / 168; 256 x 256 over 169,343 rows, 661 each, 49.5 / 58; tiles of 128 x 256, half the sums, there 47.9, over 410,003
-// rows 93, 87 so. 128 x 512 over 500,000 rows, 128 x 256 / 128 x 128: 106 / 130; 96 x 914 over 125,702 56 / 71; 120 x 300 over 1,000,000 183 / 179.)
+// rows 93, 87 so. Tiles of 128 x 256 / 128 x 128 in turn: 500,000 rows 128 x 512 106 / 132, 125,702 rows 96 x 914 52 / 54, 1,000,000 rows 120 x 300 175 / 178,
+// 200,000 rows 128 x 2048 146 / 188, 131,101 rows 65 x 256 23.9 / 23.6; 256 x 128 / 128 x 128 for the same turned round: 106 / 135, 52 / 56, 168 / 181, 145 / 193,
+// 23.5 / 23.9.)
 using Big = Tile<2, 4, 8, 4, 64>;
 using Wide = Tile<2, 4, 4, 4, 64>;
 using Tall = Tile<4, 2, 4, 4, 64>;
