@@ -524,8 +524,9 @@ int32_t varco_scaled_bwd_weight(int64_t n_rows, int32_t n_in, int32_t n_out, con
 /* Root-mean-square norm, with the residual's addition:
  *   u = x + residual, rounded to the storage type (u = x without one)     s = 1 / sqrt(mean of u^2 over the row + eps)
  *   y[j] = u[j] s gain[j]
- * in fp32, the sum of the squares too: a row whose sum fp32 cannot hold (elements from about 1e19 on) has s = 0. With eps = 0 a row of zeros has s infinite
- * and y NaN, one of elements below 2^-75 alone (no square is left) s and y infinite, and below 2^-63 (1e-19) s loses bits; an eps of 1e-30 or more hides both.
+ * squares and the sums of up to 32 of them in fp32, their sum, the mean and eps in fp64; s is rounded once to fp32, and u s gain twice. A row with
+ * elements from about 3e18 on may have s = 0. With eps = 0 a row of zeros has s infinite and y NaN, one of elements below 2^-75 alone (no square is left) s
+ * and y infinite, and below 2^-63 (1e-19) s loses bits; an eps of 1e-30 or more hides both.
  * residual, gain (fp32, NULL = 1), total, y, codes (with scales), inv_rms may be NULL; what is given is written: total = u, which
  * the backward call reads, y in the storage type, the codes of y (from its fp32 values), inv_rms[row] = s (fp32). total and y may be
  * x or the residual themselves (same leading dimension), not each other. */

@@ -39,25 +39,40 @@ __device__ __forceinline__ float other_lane(float x) {
     const int u = int(__float_as_uint(x));
     return __uint_as_float(uint32_t(__builtin_amdgcn_update_dpp(u, u, CTRL, 0xF, 0xF, false)));
 }
-template <int N, typename F>
-__device__ __forceinline__ float over_lanes(float x, F f) {
+template <int CTRL>
+__device__ __forceinline__ double other_lane(double x) {
+    const auto u = __builtin_bit_cast(uint64_t, x);
+    const auto half = [](uint32_t v) { return uint32_t(__builtin_amdgcn_update_dpp(int(v), int(v), CTRL, 0xF, 0xF, false)); };
+    return __builtin_bit_cast(double, uint64_t(half(uint32_t(u >> 32))) << 32 | half(uint32_t(u)));
+}
+// f of the numbers that the two halves of 32 (WIDE: of 64) lanes hold.
+template <bool WIDE, typename F>
+__device__ __forceinline__ float over_halves(float x, F f) {
+    const uint32_t u = __float_as_uint(x);
+    const auto r = WIDE ? __builtin_amdgcn_permlane32_swap(u, u, false, false) : __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+template <bool WIDE, typename F>
+__device__ __forceinline__ double over_halves(double x, F f) {
+    const auto u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = uint32_t(u), hi = uint32_t(u >> 32);
+    const auto r = WIDE ? __builtin_amdgcn_permlane32_swap(lo, lo, false, false) : __builtin_amdgcn_permlane16_swap(lo, lo, false, false);
+    const auto s = WIDE ? __builtin_amdgcn_permlane32_swap(hi, hi, false, false) : __builtin_amdgcn_permlane16_swap(hi, hi, false, false);
+    return f(__builtin_bit_cast(double, uint64_t(s[0]) << 32 | r[0]), __builtin_bit_cast(double, uint64_t(s[1]) << 32 | r[1]));
+}
+template <int N, typename S, typename F>
+__device__ __forceinline__ S over_lanes(S x, F f) {
     if (N >= 2) x = f(x, other_lane<0xB1>(x));          // quad_perm 1 0 3 2
     if (N >= 4) x = f(x, other_lane<0x4E>(x));          // quad_perm 2 3 0 1
     if (N >= 8) x = f(x, other_lane<0x141>(x));         // row_half_mirror: the other four lanes of eight
     if (N >= 16) x = f(x, other_lane<0x140>(x));        // row_mirror: the other eight of sixteen
-    if (N >= 32) {
-        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-        x = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
-    }
-    if (N >= 64) {
-        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-        x = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
-    }
+    if (N >= 32) x = over_halves<false>(x, f);
+    if (N >= 64) x = over_halves<true>(x, f);
     return x;
 }
-template <int N>
-__device__ __forceinline__ float lanes_sum(float x) {
-    return over_lanes<N>(x, [](float a, float b) { return a + b; });
+template <int N, typename S>
+__device__ __forceinline__ S lanes_sum(S x) {
+    return over_lanes<N>(x, [](S a, S b) { return a + b; });
 }
 template <int N>
 __device__ __forceinline__ float lanes_max(float x) {

@@ -7,6 +7,7 @@
 // backward pass 125 us (130); 2,449,029 x 512 bf16 with a residual and codes 1,940 us (2,005), 4.5 TB/s; 1,000,003 x 1000 bf16 backward 1,650 us
 // (1,625), 4.9 TB/s.
 #include <algorithm>
+#include <cfloat>
 
 #include "row_layout.h"
 #include "varco_scaled.h"
@@ -14,8 +15,8 @@
 namespace {
 
 // Sum over the G lanes of a row, in all of them, in one order.
-template <int G>
-__device__ __forceinline__ float row_sum(float x, float* shared) {
+template <int G, typename S>
+__device__ __forceinline__ S row_sum(S x, S* shared) {
     if constexpr (G <= 64) {
         return lanes_sum<G>(x);
     } else {
@@ -23,18 +24,30 @@ __device__ __forceinline__ float row_sum(float x, float* shared) {
         __syncthreads();             // (the previous row's sums have been read)
         if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = x;
         __syncthreads();
-        float s = 0.f;
+        S s = S(0);
 #pragma unroll
         for (int i = 0; i < G / 64; ++i) s += shared[i];
         return s;
     }
 }
 
+// 1 / sqrt(m), rounded once: a Newton step from the unit's root (off by a step), with its residual 1 - m h^2 in twice the bits. Where m is no normal
+// number of fp32 the root is one of fp32 throughout (infinite, 0, NaN, of few bits). The lanes' sums are added in fp64 before it: of the roundings of
+// a sum in fp32 the last few additions' count most, and with those, the root's and the division's 1 / rms was off by 0.71 2^-24 on average, 0.43 so (rounding
+// alone: 0.43), and every value made of it, codes next to a rounding's border among them.
+__device__ __forceinline__ float inverse_root(double m) {
+    const float hi = float(m);
+    if (!(hi >= FLT_MIN && hi < INFINITY)) return 1.f / sqrtf(hi);
+    const float lo = float(m - double(hi)), h = __builtin_amdgcn_rsqf(hi);
+    const float p = hi * h, q = fmaf(lo, h, fmaf(hi, h, -p));        // m h = p + q
+    return fmaf(0.5f * h, fmaf(-q, h, fmaf(-p, h, 1.f)), h);
+}
+
 template <typename T, int G, int E, bool CODES, bool ANY>
 __global__ __launch_bounds__(row_threads(G)) void rms_norm_kernel(NormFwdArgs a) {
     using Row = RowPiece<T>;
     constexpr int P = Row::P, kRows = row_threads(G) / G;
-    __shared__ float shared[G > 64 ? G / 64 : 1];
+    __shared__ double shared[G > 64 ? G / 64 : 1];
     const int t = threadIdx.x & (G - 1);
     float gain[E][P];
 #pragma unroll
@@ -44,7 +57,7 @@ __global__ __launch_bounds__(row_threads(G)) void rms_norm_kernel(NormFwdArgs a)
             const int32_t c = (t + e * G) * P + j;
             gain[e][j] = c < a.width && a.gain ? a.gain[c] : 1.f;
         }
-    const float share = 1.f / float(a.width);
+    const double share = 1.0 / double(a.width);
     for (int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / G; row < a.n_rows; row += int64_t(gridDim.x) * kRows) {
         float v[E][P];
         float sum = 0.f;
@@ -66,7 +79,7 @@ __global__ __launch_bounds__(row_threads(G)) void rms_norm_kernel(NormFwdArgs a)
         for (int e = 0; e < E; ++e)
 #pragma unroll
             for (int j = 0; j < P; ++j) sum = fmaf(v[e][j], v[e][j], sum);
-        const float s = 1.f / sqrtf(fmaf(row_sum<G>(sum, shared), share, a.eps));
+        const float s = inverse_root(fma(row_sum<G>(double(sum), shared), share, double(a.eps)));
         if (t == 0 && a.inv_rms) a.inv_rms[row] = s;
 #pragma unroll
         for (int e = 0; e < E; ++e)
