@@ -3,8 +3,8 @@
 //   h = dy g    xh = u s    dx = s (h - xh mean(h xh)) + du    dg = sum over rows of dy xh
 // One pass: a row's elements stay in registers between the sum and their use. G lanes take a row, E pieces of 16 bytes per lane;
 // rows above 2,048 elements are taken by 512 lanes, which meet in LDS.
-// Bound by reading and writing each row once: 169,343 x 256 fp32 with a residual 125 us, 5.5 TB/s (132 with stores that the caches keep), its
-// backward pass 125 us (130); 2,449,029 x 512 bf16 with a residual and codes 1,940 us (2,005), 4.5 TB/s; 1,000,003 x 1000 bf16 backward 1,650 us
+// Bound by reading and writing each row once: 169,343 x 256 fp32 with a residual 125 to 131 us, 5.5 TB/s (132 with stores that the caches keep), its
+// backward pass 125 us (130); 2,449,029 x 512 bf16 with a residual and codes 1,955 us (2,005), 4.5 TB/s; 1,000,003 x 1000 bf16 backward 1,650 us
 // (1,625), 4.9 TB/s.
 #include <algorithm>
 #include <cfloat>

@@ -6,7 +6,7 @@
 // bytes more than a multiple of 256, so that the four rows of such a block start in four different quarters of the banks.
 // The rows are cut into slabs, one workgroup per slab and tile, which leaves its sums as they lie in its accumulators; they are added by a second
 // launch in one order. (410,003 rows, 100 x 47: 26 us, 41 with the sums as matrices; 169,343 rows, 256 x 256: 49, 52.)
-// 2,449,029 rows, 512 x 512: 1,240 us, 1,040 TFLOP/s: the matrix units work 44 % of the time, the vector ALU (conversion, addresses) a third, and the
+// 2,449,029 rows, 512 x 512: 1,140 to 1,300 us, 990 to 1,130 TFLOP/s: the matrix units work 44 % of the time, the vector ALU (conversion, addresses) a third, and the
 // two wavefronts of a SIMD do the one and the other mostly at the same time. (Codes requested when they are needed, one buffer, tiles of 128 x 128: 3,260 us.
 // LDS layouts without the bank conflicts, a quarter of the cycles: 1,260 to 1,280; conversion between the products: 1,235, and 3 % slower over 256 x 256.)
 // 169,343 rows, 256 x 256: 49 us, half of it the sums of the 256 slabs, 64 MB written and read.
