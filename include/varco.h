@@ -504,13 +504,14 @@ int32_t varco_quantize_rows(int32_t dtype, int64_t n_rows, int32_t width, const 
 int32_t varco_quantize_weights(int32_t n_in, int32_t n_out, const void* h, int64_t ldh, void* turned, void* turned_scales, void* codes,
                                void* scales, varco_stream stream);
 /* c = act((c +) X W), n_rows x n_out of type dtype, X of n_rows x n_in codes, W the n_in x n_out weights given as `turned` above
- * (input gradients: X the codes of the errors, n_in the layer's outputs, W its `codes`). dtype VARCO_F32: products of the numbers that codes under
- * scales 2^-124 .. 2^119 stand for, exact, and sums as accurate as fp32 additions; under smaller scales numbers are taken to the nearest multiple of 2^-133,
- * and the code 256 under 2^120 (finite numbers from 1.9375 2^127 on become that) stands for 2^128, beyond fp32: what
- * it takes part in is infinite or NaN. VARCO_BF16: exact products
- * under all scales, sums in fp32 of the 8-bit matrix units, which drop of each product what lies 2^-13 below the
- * largest of the eight consecutive ones it is added with (an error below 2^-10 of the sum of the products' sizes, typically a tenth of the rounding
- * of c), at twice the rate. One rounding to c. act: VARCO_ACT_*. accumulate != 0 adds to what c holds. c must not overlap an operand. */
+ * (input gradients: X the codes of the errors, n_in the layer's outputs, W its `codes`). One rounding to c. act: VARCO_ACT_*. accumulate != 0 adds to what c
+ * holds. c must not overlap an operand.
+ *   VARCO_F32   exact products of the numbers that codes under scales 2^-124 .. 2^119 stand for, sums as accurate as fp32 additions. Under smaller scales
+ *               numbers are taken to the nearest multiple of 2^-133; the code 256 under 2^120 (finite numbers from 1.9375 2^127 on become that) is 2^128, beyond
+ *               fp32: what it takes part in is infinite or NaN.
+ *   VARCO_BF16  exact products under all scales, sums in fp32 of the 8-bit matrix units, which drop of each product what lies 2^-13 below the largest of the
+ *               eight consecutive ones it is added with (an error below 2^-10 of the sum of the products' sizes, typically a tenth of the rounding of c), at
+ *               twice the rate. */
 int32_t varco_scaled_transform(int32_t dtype, int64_t n_rows, int32_t n_in, int32_t n_out, const void* codes, const void* scales,
                                const void* w_codes, const void* w_scales, void* c, int64_t ldc, int32_t accumulate, int32_t act,
                                varco_stream stream);
@@ -524,7 +525,7 @@ int32_t varco_scaled_bwd_weight(int64_t n_rows, int32_t n_in, int32_t n_out, con
 /* Root-mean-square norm, with the residual's addition:
  *   u = x + residual, rounded to the storage type (u = x without one)     s = 1 / sqrt(mean of u^2 over the row + eps)
  *   y[j] = u[j] s gain[j]
- * squares and the sums of up to 32 of them in fp32, their sum, the mean and eps in fp64; s is rounded once to fp32, and u s gain twice. A row with
+ * with squares and the sums of up to 32 of them in fp32, their sum, the mean and eps in fp64; s is rounded once to fp32, and u s gain twice. A row with
  * elements from about 3e18 on may have s = 0. With eps = 0 a row of zeros has s infinite and y NaN, one of elements below 2^-75 alone (no square is left) s
  * and y infinite, and below 2^-63 (1e-19) s loses bits; an eps of 1e-30 or more hides both.
  * residual, gain (fp32, NULL = 1), total, y, codes (with scales), inv_rms may be NULL; what is given is written: total = u, which

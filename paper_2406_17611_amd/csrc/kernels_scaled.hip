@@ -330,9 +330,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void scaled_tile_kernel(ScaledArgs
 // value. (Hence not where c is added to. Reductions are whole 256: two buffers.)
 // Weight row [q1 h q0 v1 v0] (bits) of a fragment's 32 is output [q1 q0 h v1 v0] of it: accumulators 4 q + v, q = 0, 1 and 2, 3, of a lane are
 // then 8 consecutive outputs.
-// 262,181 x 2048 -> 2048: 1,110 to 1,250 us (1,760 to 1,980 TFLOP/s; random codes 1,205, rows of normal numbers 1,130); 131,072 x 8192 -> 2048 1,805 to 1,995 us, at
-// best 2,430 TFLOP/s. Tiles that start anew
-// (scaled_tile_kernel, 8 wavefronts of 128 x 64): 1,305 and 2,160. With all copies of a block in a row 1,310: a wavefront that issues
+// 262,181 x 2048 -> 2048: 1,110 to 1,250 us, 1,760 to 1,980 TFLOP/s (it varies with what is multiplied: 1,130 over rows of normal numbers, 1,205 over random
+// codes); 131,072 x 8192 -> 2048 1,805 to 1,995 us, 2,430 TFLOP/s at best. Tiles that start anew (scaled_tile_kernel, 8 wavefronts of 128 x 64): 1,305 and
+// 2,160. With all copies of a block in a row 1,310: a wavefront that issues
 // a copy waits until the one before is taken, and issues no product meanwhile. Without copies 900: what bounds it is the L2, 8.5 TB/s.
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 constexpr int kBigTile = 256, kBigBuffer = 2 * kBigTile * BK;

@@ -140,6 +140,14 @@ extern "C" int32_t varco_quantize_weights(int32_t n_in, int32_t n_out, const voi
     VARCO_CHECK(check_matrix(h, ldh, n_out, 4, true, fn));
     VARCO_CHECK(check_codes(turned, turned_scales, false, fn));
     VARCO_CHECK(check_codes(codes, scales, !turned, fn));
+    const Rows from = rows_of(h, n_in, ldh, n_out, 4);
+    const auto blocks = [](int64_t n) { return (n + kCodeBlock - 1) / kCodeBlock; };
+    const Rows written[] = {whole(turned, n_out * code_ld(n_in)), whole(turned_scales, blocks(n_out) * scale_ld(n_in)), whole(codes, n_in * code_ld(n_out)),
+                            whole(scales, blocks(n_in) * scale_ld(n_out))};
+    for (int i = 0; i < 4; ++i) {
+        VARCO_CHECK(check_written(written[i], {from}, false, fn));
+        for (int j = 0; j < i; ++j) VARCO_CHECK(check_written(written[i], {written[j]}, false, fn));
+    }
     return result(varco_launch_quantize_weights(n_in, n_out, static_cast<const float*>(h), ldh, static_cast<uint8_t*>(turned),
                                                 static_cast<uint8_t*>(turned_scales), static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scales),
                                                 static_cast<hipStream_t>(stream)), fn);

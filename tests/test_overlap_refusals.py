@@ -55,3 +55,13 @@ def test_results_of_products_over_their_operands(operand):
     at[operand] = c + 4 * LD * 4 + 384                         # the last row of c
     refused("varco_scaled_transform", [vb.F32, N, 100, W, *at, c, LD, 0, 0, None], vb.ERR_INVALID_ARG, "overlap")
     refused("varco_scaled_bwd_weight", [N, 5, W, *at, c, LD, 0, None, 0, None], vb.ERR_INVALID_ARG, "overlap")
+
+
+@pytest.mark.parametrize("which", range(4))
+@pytest.mark.parametrize("at", [X, X + 1200 * 4 + 384])
+def test_codes_of_weights_over_the_weights_or_each_other(which, at):
+    out = [FAR[0], FAR[1], FAR[2], FAR[3]]
+    out[which] = at
+    refused("varco_quantize_weights", [N, W, X, LD, *out, None], vb.ERR_INVALID_ARG, "overlap")
+    out[which] = out[which - 1]
+    refused("varco_quantize_weights", [N, W, X, LD, *out, None], vb.ERR_INVALID_ARG, "overlap")
