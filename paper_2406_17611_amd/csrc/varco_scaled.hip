@@ -50,7 +50,7 @@ Rows whole(const void* p, int64_t bytes) { return {p, 1, bytes, bytes}; }
 // Whether a byte of a is one of b. Rows as far apart (columns of one wider matrix, say) and a single row are compared row by row, others by where they begin
 // and end.
 bool overlap(const Rows& a, const Rows& b) {
-    if (!a.at || !b.at || a.n < 1 || b.n < 1) return false;
+    if (!a.at || !b.at || a.n < 1 || b.n < 1 || a.bytes < 1 || b.bytes < 1) return false;
     if (a.n > 1 && (b.n == 1 || reinterpret_cast<uintptr_t>(b.at) < reinterpret_cast<uintptr_t>(a.at))) return overlap(b, a);
     const uintptr_t start = reinterpret_cast<uintptr_t>(a.at), other = reinterpret_cast<uintptr_t>(b.at);
     if (a.n == 1) {                              // the first row of b that ends behind a's start has to begin before a's end

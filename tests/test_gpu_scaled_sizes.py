@@ -130,3 +130,18 @@ def test_a_tensor_of_more_than_two_to_the_31_elements(dtype):
     assert_within(got, f * np.array([3.0, 4.0, 12.0, 84.0]), (STEP[dtype] + 2.0 ** -23) * f * np.array([3.0, 4.0, 12.0, 84.0]), "clipped")
     big[0] = big[1 << 30] = big[n - 1] = 0
     assert not bool(big.any())
+
+
+@pytest.mark.parametrize("n_in,n_out", [(1, 1), (1, 40), (300, 47)])
+@pytest.mark.parametrize("accumulate", [0, 1])
+def test_gradients_over_no_rows_of_buffers_that_are_there(n_in, n_out, accumulate):
+    """Through the C ABI, whose callers keep their buffers when a batch is empty: before, inside and behind the gradient's memory."""
+    memory = torch.ones(1 << 16, device="cuda")
+    at = memory.data_ptr() + (1 << 17)
+    dh = memory[1 << 15:(1 << 15) + n_in * n_out]
+    for codes in (memory.data_ptr(), at, at + (1 << 16)):
+        dh.fill_(1.0)
+        code = vb.lib().varco_scaled_bwd_weight(0, n_in, n_out, codes, codes, codes, codes, at, n_out, accumulate, None, 0,
+                                                torch.cuda.current_stream().cuda_stream)
+        assert code == vb.OK and bool((dh == accumulate).all())
+    assert bool((memory[:1 << 15] == 1).all()) and bool((memory[(1 << 15) + n_in * n_out:] == 1).all())
